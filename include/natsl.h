@@ -61,12 +61,14 @@ typedef enum natsl_status {
     NATSL_ERR_UNSUPPORTED = -8, /* valid request this build does not implement */
     NATSL_ERR_TOO_LARGE = -9,   /* natsl_hybrid_fwd_static: problem needs more than the built-in scratch */
     NATSL_ERR_TIMEOUT = -10,    /* a bounded device-side wait expired (device-detected); kernel drained */
-    NATSL_ERR_ROUTE = -11       /* block-level routing: route changes inside a block, or a block end
+    NATSL_ERR_ROUTE = -11,      /* block-level routing: route changes inside a block, or a block end
                                    without the block's cache entries (device-detected) */
+    NATSL_ERR_TREE = -12        /* drafted tree: a parent that is not a lower index (or -1), a count outside
+                                   [0, L], or an accepted path that does not climb (device-detected) */
 } natsl_status;
 
 enum { NATSL_F32 = 0, NATSL_BF16 = 1 };
-enum { NATSL_OP_FWD = 0, NATSL_OP_BWD = 1, NATSL_OP_DECODE = 2, NATSL_OP_COMPACT = 3 };
+enum { NATSL_OP_FWD = 0, NATSL_OP_BWD = 1, NATSL_OP_DECODE = 2, NATSL_OP_COMPACT = 3, NATSL_OP_TREE = 4 };
 
 /* flags */
 enum {
@@ -334,6 +336,88 @@ int natsl_decode_step(const void *q, const void *k, const void *v, const float *
 int natsl_decode_block_end(const uint8_t *route_block, const float *g_block, float *state,
                            float *state_start, int32_t *cache_len, int32_t block_len,
                            const natsl_params *p, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Speculative generation: the layer over a tree of drafted tokens (Section 4.1, per-token generation; the
+ * paper generates one token at a time, which is the tree of one node).  A draft model proposes p->L tokens
+ * per sequence, 1 <= p->L <= 64, as a tree: token i follows token parent[b,i] of the same sequence, or, with
+ * -1, the context that `state` and the cache hold.  Every node gets the output that natsl_decode_step would
+ * give it after its ancestors: the delta rule runs along its path, and its softmax reads the cache and the
+ * retained tokens of its path.  Routes as in natsl_decode_step: 0 folded into the state, 1 retained, 2 both
+ * (a token of a block whose decision is open).  Nothing is updated: natsl_tree_commit does that for the path
+ * that was accepted.
+ *   q,k,v [B,L,H,d] in p->dtype; g,beta [B,L,H] fp32; route [B,L,H] u8; p->w [B,L,H,2] or NULL;
+ *   parent [B,L] i32, parent[b,i] < i: parents come before their children;
+ *   n_nodes [B] i32: nodes of each sequence's tree, or NULL for L each.  The rows behind them are neither
+ *       read nor written, in all tensors with an L;
+ *   state [B,H,d,d] fp32; k_cache,v_cache [B,H,cache_cap,d] in p->dtype; cache_len [B,H] i32: read only (a
+ *       length outside [0, cache_cap] counts as the nearer of both, and is reported as NATSL_ERR_CACHE_FULL);
+ *   out [B,L,H,d] in p->dtype;
+ *   u [B,L,H,d] fp32 or NULL: what each node adds to the state along its key, for natsl_tree_commit (zero for
+ *       route 1);
+ *   p->lse [B,H,L] ([B,H,G,L] with p->G > 1) fp32 or NULL: log-sum-exp of the softmax logits, -inf where a
+ *       node sees no key (its softmax output is then zero).
+ * p->G in {1, 2, 4} with d / G >= 32 and NATSL_QK_NORM as in natsl_decode_step.  bf16 storage runs on the
+ * tensor cores, except with NATSL_FORCE_SIMT or four softmax heads.  A parent that is not below its node
+ * counts as -1 and is reported as NATSL_ERR_TREE, like a count outside [0, L] (the nearer of both).
+ * ws holds natsl_workspace_size(p, NATSL_OP_TREE) bytes, is zero-filled once before its first use and is not
+ * shared by calls that overlap on the GPU.  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, UNSUPPORTED, CUDA.
+ */
+int natsl_tree_step(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                    const uint8_t *route, const int32_t *parent, const int32_t *n_nodes, const float *state,
+                    const void *k_cache, const void *v_cache, const int32_t *cache_len, int32_t cache_cap,
+                    void *out, float *u, const natsl_params *p, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The accepted path of a tree becomes part of the context: state and cache are then what natsl_decode_step
+ * would have left after these tokens.
+ *   k,v,g,route: as given to natsl_tree_step; u: as it left it;
+ *   path [B,L] i32: the accepted nodes from the context on, each the parent of the next (so strictly
+ *       ascending), n_path [B] i32 of them (0: nothing is accepted); the rest of path is not read;
+ *   state [B,H,d,d] fp32, k_cache,v_cache [B,H,cache_cap,d], cache_len [B,H] i32: updated in place.
+ * A (sequence, head) whose cache has no room for its retained tokens is left untouched and reported as
+ * NATSL_ERR_CACHE_FULL; a sequence whose path is not strictly ascending inside [0, L), or whose n_path lies
+ * outside [0, L], is left untouched and reported as NATSL_ERR_TREE.  ws: the tree's workspace (for the status
+ * word).  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, CUDA.
+ */
+int natsl_tree_commit(const void *k, const void *v, const float *g, const uint8_t *route, const float *u,
+                      const int32_t *path, const int32_t *n_path, float *state, void *k_cache, void *v_cache,
+                      int32_t *cache_len, int32_t cache_cap, const natsl_params *p, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/*
+ * Attention weight of the retained entries, for natsl_cache_evict (no counterpart in the paper, which keeps
+ * every softmax token): the probabilities that p->L query rows per sequence give each cache entry, summed
+ * over the rows and over the p->G softmax heads, are added to `weight`:
+ *   weight[b,h,j] += sum_t sum_s exp(scale_sm q[b,t,h,s].k_cache[b,h,j,s] - lse[b,h,s,t]),  j < visible[b,t,h].
+ *   q [B,L,H,d] in p->dtype, any L >= 1: the last queries of a prompt, the accepted nodes of a tree, ...;
+ *   lse [B,H,L] ([B,H,G,L]) fp32, as natsl_hybrid_fwd and natsl_tree_step leave it in p->lse; a row whose
+ *       value is not finite counts for nothing;
+ *   visible [B,L,H] i32: how many entries, from the first, a row sees (with the whole prompt's queries the
+ *       running sum of `route` over L), or NULL for all of them;
+ *   k_cache [B,H,cache_cap,d], cache_len [B,H]: read (a length outside [0, cache_cap] counts as the nearer of
+ *       both); weight [B,H,cache_cap] fp32: updated in place, entries from the length on are left alone.
+ * NATSL_QK_NORM and p->G as in natsl_tree_step.  No workspace.  Errors: NULL, SHAPE, DTYPE, ALIGN,
+ * UNSUPPORTED, CUDA.
+ */
+int natsl_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
+                        const int32_t *cache_len, int32_t cache_cap, float *weight, const natsl_params *p,
+                        void *stream);
+
+/*
+ * Eviction: every (sequence, head) with more than `keep` entries keeps `keep` of them -- the first `first`,
+ * the last `recent` and, of those between, the ones of the highest weight (ties: the lower index; a NaN
+ * counts as the lowest weight) -- moved to the front in their order; cache_len becomes `keep`.  Others are
+ * left untouched.
+ *   k_cache,v_cache [B,H,cache_cap,d] in p->dtype, weight [B,H,cache_cap] fp32, cache_len [B,H] i32: updated
+ *       in place; rows from the new length on are left as they were;
+ *   kept [B,H,keep] i32: the former places of the entries that are now 0 .. cache_len - 1.
+ * 1 <= keep <= cache_cap, first >= 0, recent >= 0, first + recent <= keep.  Of p only B, H, d, C, dtype, eps
+ * count (the last two must be valid).  No workspace.  Errors: NULL, SHAPE, DTYPE, ALIGN, CUDA.
+ */
+int natsl_cache_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int32_t cache_cap,
+                      int32_t keep, int32_t first, int32_t recent, int32_t *kept, const natsl_params *p,
+                      void *stream);
 
 /* Synchronises `stream`, returns (and clears) the status word kernels wrote at ws[0]. */
 int natsl_device_status(void *ws, void *stream);

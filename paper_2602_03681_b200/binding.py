@@ -16,7 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libnatsl.so")
 
 NATSL_F32, NATSL_BF16 = 0, 1
-OP_FWD, OP_BWD, OP_DECODE, OP_COMPACT = 0, 1, 2, 3
+OP_FWD, OP_BWD, OP_DECODE, OP_COMPACT, OP_TREE = 0, 1, 2, 3, 4
 FORCE_SIMT = 1
 SINGLE_PASS_SCAN = 2
 BLOCK_ROUTING = 4
@@ -28,11 +28,13 @@ QK_NORM = 128
 ERR_CACHE_FULL = -7
 ERR_UNSUPPORTED = -8
 ERR_ROUTE = -11
+ERR_TREE = -12
 
 EXPORTS = ["natsl_workspace_size", "natsl_route_compact", "natsl_hybrid_fwd", "natsl_hybrid_bwd",
            "natsl_decode_step", "natsl_decode_block_end", "natsl_device_status", "natsl_hybrid_fwd_static",
            "natsl_score_layer", "natsl_static_status", "natsl_debug_set_wait_limit",
-           "natsl_stage_name", "natsl_launch_count", "natsl_strerror"]
+           "natsl_stage_name", "natsl_launch_count", "natsl_strerror", "natsl_tree_step", "natsl_tree_commit",
+           "natsl_cache_weights", "natsl_cache_evict"]
 ERR_TIMEOUT = -10
 ERR_TOO_LARGE = -9
 STATIC_WS_BYTES = 32 << 20
@@ -87,7 +89,7 @@ def lib() -> ctypes.CDLL:
         _lib.natsl_stage_name.restype = ctypes.c_char_p
         _lib.natsl_stage_name.argtypes = [ctypes.c_int, ctypes.c_int]
         _lib.natsl_launch_count.restype = ctypes.c_uint64
-        for name in EXPORTS[:7] + ["natsl_score_layer", "natsl_static_status"]:
+        for name in EXPORTS[:7] + EXPORTS[-4:] + ["natsl_score_layer", "natsl_static_status"]:
             getattr(_lib, name).restype = ctypes.c_int
         _lib.natsl_debug_set_wait_limit.restype = None
         _lib.natsl_debug_set_wait_limit.argtypes = [ctypes.c_uint32, ctypes.c_int]
@@ -216,6 +218,32 @@ def natsl_decode_block_end(route_block, g_block, state, state_start, cache_len, 
 
 def natsl_score_layer(x, w_score, scores, route, p: natsl_params):
     rc = (_py or _native()).score_layer(x, w_score, scores, route, p)
+    if rc:
+        _check(rc)
+
+
+def natsl_tree_step(q, k, v, g, beta, route, parent, n_nodes, state, k_cache, v_cache, cache_len, out, u,
+                    p: natsl_params, ws):
+    rc = (_py or _native()).tree_step(q, k, v, g, beta, route, parent, n_nodes, state, k_cache, v_cache, cache_len, out,
+                                      u, p, ws)
+    if rc:
+        _check(rc)
+
+
+def natsl_tree_commit(k, v, g, route, u, path, n_path, state, k_cache, v_cache, cache_len, p: natsl_params, ws):
+    rc = (_py or _native()).tree_commit(k, v, g, route, u, path, n_path, state, k_cache, v_cache, cache_len, p, ws)
+    if rc:
+        _check(rc)
+
+
+def natsl_cache_weights(q, lse, visible, k_cache, cache_len, weight, p: natsl_params):
+    rc = (_py or _native()).cache_weights(q, lse, visible, k_cache, cache_len, weight, p)
+    if rc:
+        _check(rc)
+
+
+def natsl_cache_evict(k_cache, v_cache, weight, cache_len, keep, first, recent, kept, p: natsl_params):
+    rc = (_py or _native()).cache_evict(k_cache, v_cache, weight, cache_len, keep, first, recent, kept, p)
     if rc:
         _check(rc)
 

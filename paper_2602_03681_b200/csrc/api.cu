@@ -75,6 +75,18 @@ struct FwdWs {
     size_t bytes;
 };
 
+constexpr int kTreeNodes = 64;   // nodes of a drafted tree: a machine word of ancestors each
+
+// Softmax heads per linear head in generation: any slices of 32 columns or more.
+bool generation_groups(const natsl_params *p) {
+    const int G = head_groups(p).G;
+    return G == 1 || ((G == 2 || G == 4) && p->d / G >= 32);
+}
+// A cache's rows, and blocks of them over all pairs, are counted in 31 bits.
+bool cache_fits(const natsl_params *p, int32_t cap) {
+    return cap > 0 && (long long)p->B * p->H <= 0x7fffffff / 65 && (long long)p->B * p->H * ((cap + 15LL) / 16) <= 0x7fffffff;
+}
+
 bool use_tensor_cores(const natsl_params *p) {
     return p->dtype == NATSL_BF16 && !(p->flags & NATSL_FORCE_SIMT);
 }
@@ -405,6 +417,7 @@ const char *natsl_stage_name(int op, int i) {
                                 "softmax_combine"};
     if (op == NATSL_OP_FWD && i >= 0 && i < 4) return fwd[i];
     if (op == NATSL_OP_DECODE && i == 0) return "decode_step";
+    if (op == NATSL_OP_TREE && i == 0) return "tree_step";
     return nullptr;
 }
 
@@ -420,6 +433,7 @@ const char *natsl_strerror(int status) {
         case NATSL_ERR_CACHE_FULL: return "retained-KV cache full";
         case NATSL_ERR_UNSUPPORTED: return "request not implemented in this build";
         case NATSL_ERR_ROUTE: return "block-level routing: route changes inside a block";
+        case NATSL_ERR_TREE: return "drafted tree: a parent or a path that does not climb, or a count out of range";
         case NATSL_ERR_TIMEOUT: return "a bounded device-side wait expired";
         case NATSL_ERR_TOO_LARGE: return "problem needs more scratch than the library's built-in array (NATSL_STATIC_WS_BYTES)";
         default: return "unknown natsl status";
@@ -428,9 +442,13 @@ const char *natsl_strerror(int status) {
 
 int natsl_workspace_size(const natsl_params *p, int op, size_t *bytes) {
     if (!bytes) return NATSL_ERR_NULL;
-    int rc = check_params(p, op != NATSL_OP_DECODE);
+    int rc = check_params(p, op != NATSL_OP_DECODE && op != NATSL_OP_TREE);
     if (rc != NATSL_OK) return rc;
     switch (op) {
+        case NATSL_OP_TREE:
+            if (p->L < 1 || p->L > kTreeNodes) return NATSL_ERR_SHAPE;
+            *bytes = tree_workspace_bytes(p->B, p->H, p->L, p->d);
+            return NATSL_OK;
         case NATSL_OP_FWD: *bytes = carve_fwd(p, nullptr).bytes; return NATSL_OK;
         case NATSL_OP_BWD: *bytes = carve_bwd(p, nullptr).bytes; return NATSL_OK;
         case NATSL_OP_DECODE: *bytes = decode_workspace_bytes(p->B, p->H, p->d); return NATSL_OK;
@@ -826,6 +844,73 @@ int natsl_decode_block_end(const uint8_t *route_block, const float *g_block, flo
     cudaError_t e = launch_decode_block_end(route_block, g_block, state, state_start, cache_len,
                                             block_len, ws, shape_of(p),
                                             static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? NATSL_OK : NATSL_ERR_CUDA;
+}
+
+int natsl_tree_step(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                    const uint8_t *route, const int32_t *parent, const int32_t *n_nodes, const float *state,
+                    const void *k_cache, const void *v_cache, const int32_t *cache_len, int32_t cache_cap,
+                    void *out, float *u, const natsl_params *p, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_params(p, false);
+    if (rc != NATSL_OK) return rc;
+    if (!q || !k || !v || !g || !beta || !route || !parent || !state || !k_cache || !v_cache || !cache_len || !out)
+        return NATSL_ERR_NULL;
+    if (p->L < 1 || p->L > kTreeNodes || !cache_fits(p, cache_cap)) return NATSL_ERR_SHAPE;
+    if (!generation_groups(p)) return NATSL_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(u) || !aligned16(state) ||
+        !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(ws))
+        return NATSL_ERR_ALIGN;
+    if (!ws || ws_bytes < tree_workspace_bytes(p->B, p->H, p->L, p->d)) return NATSL_ERR_WORKSPACE;
+    const TreeCall c{q, k, v, g, beta, route, parent, n_nodes, p->w, state, k_cache, v_cache, cache_len, cache_cap,
+                     out, u, p->lse, p->scale_la, p->scale_sm, p->eps, ws};
+    cudaError_t e = launch_tree_step(c, shape_of(p), head_groups(p), use_tensor_cores(p), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? NATSL_OK : NATSL_ERR_CUDA;
+}
+
+int natsl_tree_commit(const void *k, const void *v, const float *g, const uint8_t *route, const float *u,
+                      const int32_t *path, const int32_t *n_path, float *state, void *k_cache, void *v_cache,
+                      int32_t *cache_len, int32_t cache_cap, const natsl_params *p, void *ws, size_t ws_bytes,
+                      void *stream) {
+    int rc = check_params(p, false);
+    if (rc != NATSL_OK) return rc;
+    if (!k || !v || !g || !route || !u || !path || !n_path || !state || !k_cache || !v_cache || !cache_len)
+        return NATSL_ERR_NULL;
+    if (p->L < 1 || p->L > kTreeNodes || !cache_fits(p, cache_cap)) return NATSL_ERR_SHAPE;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(u) || !aligned16(state) || !aligned16(k_cache) ||
+        !aligned16(v_cache) || !aligned16(ws))
+        return NATSL_ERR_ALIGN;
+    if (!ws || ws_bytes < tree_workspace_bytes(p->B, p->H, p->L, p->d)) return NATSL_ERR_WORKSPACE;
+    cudaError_t e = launch_tree_commit(k, v, g, route, u, path, n_path, state, k_cache, v_cache, cache_len, cache_cap,
+                                       shape_of(p), head_groups(p).norm_eps, ws, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? NATSL_OK : NATSL_ERR_CUDA;
+}
+
+int natsl_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
+                        const int32_t *cache_len, int32_t cache_cap, float *weight, const natsl_params *p,
+                        void *stream) {
+    int rc = check_params(p, false);
+    if (rc != NATSL_OK) return rc;
+    if (!q || !lse || !k_cache || !cache_len || !weight) return NATSL_ERR_NULL;
+    if (p->L < 1 || !cache_fits(p, cache_cap)) return NATSL_ERR_SHAPE;
+    if (!generation_groups(p)) return NATSL_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k_cache)) return NATSL_ERR_ALIGN;
+    cudaError_t e = launch_cache_weights(q, lse, visible, k_cache, cache_len, cache_cap, weight, p->scale_sm, shape_of(p),
+                                         head_groups(p), use_tensor_cores(p), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? NATSL_OK : NATSL_ERR_CUDA;
+}
+
+int natsl_cache_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int32_t cache_cap,
+                      int32_t keep, int32_t first, int32_t recent, int32_t *kept, const natsl_params *p,
+                      void *stream) {
+    int rc = check_params(p, false);
+    if (rc != NATSL_OK) return rc;
+    if (!k_cache || !v_cache || !weight || !cache_len || !kept) return NATSL_ERR_NULL;
+    if (!cache_fits(p, cache_cap) || keep < 1 || keep > cache_cap || first < 0 || recent < 0 ||
+        (long long)first + recent > keep)
+        return NATSL_ERR_SHAPE;
+    if (!aligned16(k_cache) || !aligned16(v_cache)) return NATSL_ERR_ALIGN;
+    cudaError_t e = launch_cache_evict(k_cache, v_cache, weight, cache_len, cache_cap, keep, first, recent, kept,
+                                       shape_of(p), static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? NATSL_OK : NATSL_ERR_CUDA;
 }
 

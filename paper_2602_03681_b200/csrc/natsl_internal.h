@@ -343,4 +343,34 @@ cudaError_t launch_decode_block_end(const uint8_t *route_block, const float *g_b
                                     float *state_start, int32_t *cache_len, int32_t block_len,
                                     void *ws, Shape s, cudaStream_t st);
 
+// tree_tc.cu, tree_simt.cu -- the layer over a tree of drafted tokens; s.L: nodes per tree (at most 64)
+struct TreeCall {
+    const void *q, *k, *v;
+    const float *g, *beta;
+    const uint8_t *route;
+    const int32_t *parent, *n_nodes;
+    const float *w, *state;
+    const void *k_cache, *v_cache;
+    const int32_t *cache_len;
+    int cap;
+    void *out;
+    float *u, *lse;
+    float scale_la, scale_sm, eps;
+    void *ws;
+};
+// Status word, per-pair tickets, linear read-outs, partial results.  Zero-filled once by the caller; the kernels leave the
+// tickets at zero.
+size_t tree_workspace_bytes(int B, int H, int T, int d);
+cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool tensor_cores, cudaStream_t st);
+// tree_commit.cu
+cudaError_t launch_tree_commit(const void *k, const void *v, const float *g, const uint8_t *route, const float *u,
+                               const int32_t *path, const int32_t *n_path, float *state, void *k_cache, void *v_cache,
+                               int32_t *cache_len, int cap, Shape s, float norm_eps, void *ws, cudaStream_t st);
+// cache_evict.cu
+cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
+                                 const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg,
+                                 bool tensor_cores, cudaStream_t st);
+cudaError_t launch_cache_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first,
+                               int recent, int32_t *kept, Shape s, cudaStream_t st);
+
 }  // namespace natsl

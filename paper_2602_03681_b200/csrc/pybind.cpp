@@ -174,10 +174,73 @@ PyObject *score_layer(PyObject *, PyObject *const *v, Py_ssize_t n) {
     NATSL_CALL(natsl_score_layer(x, w, scores, route, d_model, p, st));
 }
 
+PyObject *tree_step(PyObject *, PyObject *const *v, Py_ssize_t n) {
+    if (!count_is(n, 16)) return nullptr;
+    Args a{v};
+    const void *q = a.ptr<void>(0), *k = a.ptr<void>(1), *vv = a.ptr<void>(2);
+    const float *g = a.ptr<float>(3), *beta = a.ptr<float>(4);
+    const uint8_t *route = a.ptr<uint8_t>(5);
+    const int32_t *parent = a.ptr<int32_t>(6), *nodes = a.ptr<int32_t>(7);
+    const float *state = a.ptr<float>(8);
+    const void *kc = a.ptr<void>(9), *vc = a.ptr<void>(10);
+    const int32_t *len = a.ptr<int32_t>(11);
+    const int32_t cap = (int32_t)a.size(9, 2);
+    void *out = a.ptr<void>(12), *ws = a.ptr<void>(15);
+    float *u = a.ptr<float>(13);
+    const natsl_params *p = a.params(14);
+    const size_t wb = a.numel(15);
+    NATSL_CALL(natsl_tree_step(q, k, vv, g, beta, route, parent, nodes, state, kc, vc, len, cap, out, u, p, ws, wb, st));
+}
+
+PyObject *tree_commit(PyObject *, PyObject *const *v, Py_ssize_t n) {
+    if (!count_is(n, 13)) return nullptr;
+    Args a{v};
+    const void *k = a.ptr<void>(0), *vv = a.ptr<void>(1);
+    const float *g = a.ptr<float>(2);
+    const uint8_t *route = a.ptr<uint8_t>(3);
+    const float *u = a.ptr<float>(4);
+    const int32_t *path = a.ptr<int32_t>(5), *n_path = a.ptr<int32_t>(6);
+    float *state = a.ptr<float>(7);
+    void *kc = a.ptr<void>(8), *vc = a.ptr<void>(9), *ws = a.ptr<void>(12);
+    int32_t *len = a.ptr<int32_t>(10);
+    const int32_t cap = (int32_t)a.size(8, 2);
+    const natsl_params *p = a.params(11);
+    const size_t wb = a.numel(12);
+    NATSL_CALL(natsl_tree_commit(k, vv, g, route, u, path, n_path, state, kc, vc, len, cap, p, ws, wb, st));
+}
+
+PyObject *cache_weights(PyObject *, PyObject *const *v, Py_ssize_t n) {
+    if (!count_is(n, 7)) return nullptr;
+    Args a{v};
+    const void *q = a.ptr<void>(0);
+    const float *lse = a.ptr<float>(1);
+    const int32_t *visible = a.ptr<int32_t>(2);
+    const void *kc = a.ptr<void>(3);
+    const int32_t *len = a.ptr<int32_t>(4);
+    float *weight = a.ptr<float>(5);
+    const int32_t cap = (int32_t)a.size(3, 2);
+    const natsl_params *p = a.params(6);
+    NATSL_CALL(natsl_cache_weights(q, lse, visible, kc, len, cap, weight, p, st));
+}
+
+PyObject *cache_evict(PyObject *, PyObject *const *v, Py_ssize_t n) {
+    if (!count_is(n, 9)) return nullptr;
+    Args a{v};
+    void *kc = a.ptr<void>(0), *vc = a.ptr<void>(1);
+    float *weight = a.ptr<float>(2);
+    int32_t *len = a.ptr<int32_t>(3);
+    const int32_t cap = (int32_t)a.size(0, 2);
+    const int32_t keep = (int32_t)a.integer(4), first = (int32_t)a.integer(5), recent = (int32_t)a.integer(6);
+    int32_t *kept = a.ptr<int32_t>(7);
+    const natsl_params *p = a.params(8);
+    NATSL_CALL(natsl_cache_evict(kc, vc, weight, len, cap, keep, first, recent, kept, p, st));
+}
+
 PyMethodDef kMethods[] = {
 #define NATSL_DEF(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
     NATSL_DEF(hybrid_fwd), NATSL_DEF(hybrid_fwd_static), NATSL_DEF(hybrid_bwd), NATSL_DEF(decode_step),
-    NATSL_DEF(decode_block_end), NATSL_DEF(score_layer), {nullptr, nullptr, 0, nullptr}};
+    NATSL_DEF(decode_block_end), NATSL_DEF(score_layer), NATSL_DEF(tree_step), NATSL_DEF(tree_commit),
+    NATSL_DEF(cache_weights), NATSL_DEF(cache_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_natsl_py", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

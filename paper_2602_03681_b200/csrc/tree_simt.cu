@@ -1,0 +1,315 @@
+// Tree step on fp32 CUDA cores: the hybrid layer over a tree of up to 64 drafted tokens (Section 4.1's generation with both
+// hidden states kept; fp32 storage, NATSL_FORCE_SIMT, and four softmax heads per linear head).
+//
+// Along the path of a node the recurrence of Section 4.3 unrolls as in a chunk of the chunkwise form, with "ancestor" in the
+// place of "earlier": with D_ij the decay on the path from j (exclusive) to i and D_i the one from the context,
+//   u_i = beta_i (v_i - D_i k_i S0 - sum_{j above i, folded} D_ij (k_i.k_j) u_j)
+//   o_la_i = scale_la (D_i q_i S0 + sum_{j above or i, folded} D_ij (q_i.k_j) u_j),
+// so the state is read once and never written, and the tokens' own products form two T x T tables.  Sums over ancestors
+// run over the set bits of the node's ancestor word: a sibling's infinity or NaN cannot reach a node through 0 * inf.
+//
+// A pair's work is cut into cache items (slices of the retained K/V) and one tree item (linear branch, the tree's own
+// part of the softmax); the last of them to finish joins the partial results.  Bound by the fp32 pipes.
+#include <algorithm>
+#include "tree_common.cuh"
+
+namespace natsl {
+namespace {
+
+using namespace tree;
+
+constexpr int kKeys = 32;                         // keys per tile: one per lane
+constexpr int kWarps = kThreads / 32;
+
+__host__ __device__ inline int tree_floats(int T, int D, int G) { return 2 * T * (D + 4) + T * D + (2 + G) * T * T; }
+__host__ __device__ inline int cache_floats(int TT, int D, int G) {
+    return TT * (D + 4) + kKeys * (D + 4) + kKeys * D + G * TT * kKeys + 3 * G * TT + G * kKeys;
+}
+
+// One cache item.  Lane = key for the logits (a warp owns whole rows of a tile, so maximum and sum are shuffles), thread =
+// column for the products with V (RC rows of accumulators).
+template <typename ST, int D, int TT>
+__device__ void cache_item(const Args &a, float *sm, int b, int h, int part, int n_nodes, const Cut &c) {
+    constexpr int RC = TT * D / 128, P = D + 4;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G;
+    const int bh = b * a.H + h;
+    float *sq = sm, *sk = sq + TT * P, *sv = sk + kKeys * P, *sp = sv + kKeys * D, *s_m = sp + G * TT * kKeys,
+          *s_z = s_m + G * TT, *s_f = s_z + G * TT, *s_rk = s_f + G * TT;
+    for (int i = tid; i < TT * D; i += kThreads) {
+        const int t = i / D, x = i - t * D;
+        sq[t * P + x] = t < n_nodes ? to_f32(reinterpret_cast<const ST *>(a.q)[(((size_t)b * a.T + t) * a.H + h) * D + x]) : 0.f;
+    }
+    for (int i = tid; i < G * TT; i += kThreads) { s_m[i] = -INFINITY; s_z[i] = 0.f; }
+    __syncthreads();
+    for (int i = tid; i < G * TT; i += kThreads) {   // logits in base-2 units: scale and the row's RMS factor on q
+        const int g = i / TT, t = i - g * TT;
+        float *row = sq + t * P + g * ds, f = a.scale_sm * kLog2e;
+        if (a.norm_eps >= 0.f) {
+            float s = 0.f;
+            for (int x = 0; x < ds; ++x) s = fmaf(row[x], row[x], s);
+            f *= rsqrtf(s / ds + a.norm_eps);
+        }
+        for (int x = 0; x < ds; ++x) row[x] *= f;
+    }
+    const int col = tid % D, r0 = tid / D * RC, gc = col / ds;
+    float acc[RC];
+#pragma unroll
+    for (int r = 0; r < RC; ++r) acc[r] = 0.f;
+    const ST *kc = reinterpret_cast<const ST *>(a.k_cache) + (size_t)bh * a.cap * D;
+    const ST *vc = reinterpret_cast<const ST *>(a.v_cache) + (size_t)bh * a.cap * D;
+    const int from = part * c.tpp * kTileKeys, to = min(c.n, from + c.tpp * kTileKeys);
+    for (int j0 = from; j0 < to; j0 += kKeys) {
+        __syncthreads();                          // (the tile before has been read)
+        for (int i = tid; i < kKeys * D / 4; i += kThreads) {
+            const int j = i / (D / 4), x = (i - j * (D / 4)) * 4;
+            const bool in = j0 + j < to;          // rows past the end count as zeros: what lies there may be anything
+            const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+            *reinterpret_cast<float4 *>(sk + j * P + x) = in ? load4(kc + (size_t)(j0 + j) * D + x) : zero;
+            *reinterpret_cast<float4 *>(sv + j * D + x) = in ? load4(vc + (size_t)(j0 + j) * D + x) : zero;
+        }
+        __syncthreads();
+        if (a.norm_eps >= 0.f) {
+            for (int i = tid; i < G * kKeys; i += kThreads) {
+                const float *row = sk + (i % kKeys) * P + i / kKeys * ds;
+                float s = 0.f;
+                for (int x = 0; x < ds; ++x) s = fmaf(row[x], row[x], s);
+                s_rk[i] = rsqrtf(s / ds + a.norm_eps);
+            }
+            __syncthreads();
+        }
+        const bool seen = j0 + lane < to;
+        for (int t = warp * 4; t < TT; t += kWarps * 4) {
+            if (t >= n_nodes) break;
+            for (int g = 0; g < G; ++g) {
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int x = g * ds; x < (g + 1) * ds; x += 4) {
+                    const float4 kk = *reinterpret_cast<const float4 *>(sk + lane * P + x);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float4 qq = *reinterpret_cast<const float4 *>(sq + (t + r) * P + x);
+                        s[r] = fmaf(qq.x, kk.x, fmaf(qq.y, kk.y, fmaf(qq.z, kk.z, fmaf(qq.w, kk.w, s[r]))));
+                    }
+                }
+                const float f = a.norm_eps >= 0.f ? s_rk[g * kKeys + lane] : 1.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = g * TT + t + r;
+                    const float x = seen ? s[r] * f : -INFINITY, m0 = s_m[at], m1 = fmaxf(m0, warp_max(x));
+                    const float mu = m1 == -INFINITY ? 0.f : m1;
+                    const float p = tc::ex2_ftz(x - mu), e = tc::ex2_ftz(m0 - mu), z = warp_sum(p);
+                    sp[at * kKeys + lane] = p;
+                    __syncwarp();
+                    if (lane == 0) { s_m[at] = m1; s_f[at] = e; s_z[at] = fmaf(s_z[at], e, z); }
+                    __syncwarp();
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RC; ++r)
+            if (r0 + r < n_nodes) acc[r] *= s_f[gc * TT + r0 + r];
+        for (int j = 0; j < kKeys; j += 4) {
+            float vv[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) vv[x] = sv[(j + x) * D + col];
+#pragma unroll
+            for (int r = 0; r < RC; ++r) {
+                if (r0 + r >= n_nodes) break;
+                const float4 p = *reinterpret_cast<const float4 *>(sp + (gc * TT + r0 + r) * kKeys + j);
+                acc[r] = fmaf(p.x, vv[0], fmaf(p.y, vv[1], fmaf(p.z, vv[2], fmaf(p.w, vv[3], acc[r]))));
+            }
+        }
+    }
+    __syncthreads();
+    float *pp = reinterpret_cast<float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
+                (size_t)bh * pair_floats(a.T, D, a.parts) + (size_t)a.T * D + part * part_floats(a.T, D);
+    for (int i = tid; i < G * TT; i += kThreads) {
+        const int g = i / TT, t = i - g * TT;
+        if (t < n_nodes) { pp[g * a.T + t] = s_m[i]; pp[(4 + g) * a.T + t] = s_z[i]; }
+    }
+#pragma unroll
+    for (int r = 0; r < RC; ++r)
+        if (r0 + r < n_nodes) pp[8 * a.T + (size_t)(r0 + r) * D + col] = acc[r];
+}
+
+// The tree item: linear branch and the tree's own part of the softmax.
+template <typename ST, int D>
+__device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int n) {
+    constexpr int P = D + 4;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G, T = a.T;
+    const int bh = b * a.H + h;
+    float *sq = sm, *sk = sq + T * P, *su = sk + T * P, *sa = su + T * D, *sb = sa + T * T, *sp = sb + T * T;
+    const ST *v = reinterpret_cast<const ST *>(a.v) + ((size_t)b * T * a.H + h) * D;      // row t: v + t H D
+    for (int i = tid; i < n * D; i += kThreads) {
+        const int t = i / D, x = i - t * D;
+        const size_t at = (((size_t)b * T + t) * a.H + h) * D + x;
+        sq[t * P + x] = to_f32(reinterpret_cast<const ST *>(a.q)[at]);
+        sk[t * P + x] = to_f32(reinterpret_cast<const ST *>(a.k)[at]);
+    }
+    read_nodes(a, b, h, n, nd, sb, T);
+    __syncthreads();
+    for (int t = warp; t < n; t += kWarps) {      // the rows' norms: lanes of a softmax head's columns together
+        float xq = 0.f, xk = 0.f;
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) {
+            const float y = sq[t * P + lane * (D / 32) + x], z = sk[t * P + lane * (D / 32) + x];
+            xq = fmaf(y, y, xq);
+            xk = fmaf(z, z, xk);
+        }
+        const int ls = 32 / G;
+        for (int s = ls / 2; s > 0; s >>= 1) {
+            xq += __shfl_xor_sync(0xffffffffu, xq, s);
+            xk += __shfl_xor_sync(0xffffffffu, xk, s);
+        }
+        const bool nrm = a.norm_eps >= 0.f;
+        if (lane % ls == 0) {
+            nd->rq_sm[lane / ls][t] = nrm ? rsqrtf(xq / ds + a.norm_eps) : 1.f;
+            nd->rk_sm[lane / ls][t] = nrm ? rsqrtf(xk / ds + a.norm_eps) : 1.f;
+        }
+        for (int s = ls; s < 32; s <<= 1) {
+            xq += __shfl_xor_sync(0xffffffffu, xq, s);
+            xk += __shfl_xor_sync(0xffffffffu, xk, s);
+        }
+        if (lane == 0) {
+            nd->rq_la[t] = nrm ? rsqrtf(xq + a.norm_eps) : 1.f;
+            nd->rk_la[t] = nrm ? rsqrtf(xk + a.norm_eps) : 1.f;
+        }
+    }
+    __syncthreads();
+    // k S0 and q S0: thread = column, eight rows at a time; d = 64: two threads share a column, every other group of rows
+    float *base = reinterpret_cast<float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
+                  (size_t)bh * pair_floats(T, D, a.parts);
+    const int col = tid % D, side = tid / D;
+    const float *S = a.state + (size_t)bh * D * D + col;
+    for (int t0 = side * 8; t0 < n; t0 += 8 * kThreads / D) {
+        float ak[8], aq[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) ak[r] = aq[r] = 0.f;
+        for (int x = 0; x < D; x += 4) {
+            const float s0 = S[(size_t)x * D], s1 = S[(size_t)(x + 1) * D], s2 = S[(size_t)(x + 2) * D], s3 = S[(size_t)(x + 3) * D];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int t = min(t0 + r, n - 1);
+                const float4 kk = *reinterpret_cast<const float4 *>(sk + t * P + x), qq = *reinterpret_cast<const float4 *>(sq + t * P + x);
+                ak[r] = fmaf(kk.x, s0, fmaf(kk.y, s1, fmaf(kk.z, s2, fmaf(kk.w, s3, ak[r]))));
+                aq[r] = fmaf(qq.x, s0, fmaf(qq.y, s1, fmaf(qq.z, s2, fmaf(qq.w, s3, aq[r]))));
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const int t = t0 + r;
+            if (t >= n) break;
+            su[t * D + col] = nd->beta[t] * (to_f32(v[(size_t)t * a.H * D + col]) - nd->whole[t] * nd->rk_la[t] * ak[r]);
+            base[(size_t)t * D + col] = a.scale_la * nd->whole[t] * nd->rq_la[t] * aq[r];
+        }
+    }
+    // the tables, where j is above i or i itself (sb holds the decays)
+    for (int i = tid; i < n * n; i += kThreads) {
+        const int t = i / n, j = i - t * n;
+        if (j > t || !((nd->above[t] | 1ull << t) >> j & 1)) continue;
+        float kk = 0.f, qk = 0.f;
+        for (int g = 0; g < G; ++g) {
+            float qg = 0.f;
+            for (int x = g * ds; x < (g + 1) * ds; x += 4) {
+                const float4 y = *reinterpret_cast<const float4 *>(sk + j * P + x), q4 = *reinterpret_cast<const float4 *>(sq + t * P + x),
+                             k4 = *reinterpret_cast<const float4 *>(sk + t * P + x);
+                qg = fmaf(q4.x, y.x, fmaf(q4.y, y.y, fmaf(q4.z, y.z, fmaf(q4.w, y.w, qg))));
+                kk = fmaf(k4.x, y.x, fmaf(k4.y, y.y, fmaf(k4.z, y.z, fmaf(k4.w, y.w, kk))));
+            }
+            sp[(g * T + t) * T + j] = a.scale_sm * kLog2e * nd->rq_sm[g][t] * nd->rk_sm[g][j] * qg;
+            qk += qg;
+        }
+        const float dec = sb[t * T + j];
+        sa[t * T + j] = nd->beta[t] * dec * nd->rk_la[t] * nd->rk_la[j] * kk;
+        sb[t * T + j] = a.scale_la * dec * nd->rq_la[t] * nd->rk_la[j] * qk;
+    }
+    __syncthreads();
+    float *own = base + (size_t)T * D + a.parts * part_floats(T, D);
+    for (int i = tid; i < G * n; i += kThreads) {  // the softmax over the kept nodes of the path
+        const int g = i / n, t = i - g * n;
+        float m = -INFINITY, z = 0.f;
+        const unsigned long long seen = (nd->above[t] | 1ull << t) & nd->keep;
+        float *row = sp + (g * T + t) * T;
+        for (unsigned long long w = seen; w; w &= w - 1) m = fmaxf(m, row[__ffsll(w) - 1]);
+        const float mu = m == -INFINITY ? 0.f : m;      // (every logit -inf or NaN)
+        for (unsigned long long w = seen; w; w &= w - 1) {
+            const int j = __ffsll(w) - 1;
+            z += row[j] = tc::ex2_ftz(row[j] - mu);
+        }
+        own[g * T + t] = m;
+        own[(4 + g) * T + t] = z;
+    }
+    __syncthreads();
+    // up the tree node by node; a column's thread needs no other column
+    if (tid < D) {
+        const int gc = col / ds;
+        for (int t = 0; t < n; ++t) {
+            float u = su[t * D + col], o = base[(size_t)t * D + col], s = 0.f;
+            for (unsigned long long w = nd->above[t]; w; w &= w - 1) {
+                const int j = __ffsll(w) - 1;
+                if (nd->fold >> j & 1) {
+                    const float x = su[j * D + col];
+                    u = fmaf(-sa[t * T + j], x, u);
+                    o = fmaf(sb[t * T + j], x, o);
+                }
+                if (nd->keep >> j & 1) s = fmaf(sp[(gc * T + t) * T + j], to_f32(v[(size_t)j * a.H * D + col]), s);
+            }
+            if (nd->fold >> t & 1) o = fmaf(sb[t * T + t], u, o);
+            else u = 0.f;
+            if (nd->keep >> t & 1) s = fmaf(sp[(gc * T + t) * T + t], to_f32(v[(size_t)t * a.H * D + col]), s);
+            su[t * D + col] = u;
+            base[(size_t)t * D + col] = o;
+            own[8 * T + (size_t)t * D + col] = s;
+            if (a.u) a.u[(((size_t)b * T + t) * a.H + h) * D + col] = u;
+        }
+    }
+}
+
+template <typename ST, int D, int TT>
+__global__ void __launch_bounds__(kThreads) tree_simt_kernel(Args a) {
+    extern __shared__ __align__(16) float dyn[];
+    __shared__ Nodes nodes;
+    const int per_pair = a.parts + 1, bh = blockIdx.x / per_pair, part = blockIdx.x - bh * per_pair - 1;   // part -1: the tree
+    const int b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
+    if (part < 0) {
+        tree_item<ST, D>(a, dyn, &nodes, b, h, n);
+    } else {
+        const Cut c = cut_of(a.cache_len[bh], a.cap, a.parts, a.least_tiles);
+        if (part < c.np) cache_item<ST, D, TT>(a, dyn, b, h, part, n, c);
+    }
+    if (last_of_pair(a, bh)) join_pair<ST, D>(a, b, h, n);
+}
+
+template <typename ST, int D, int TT>
+cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
+    const auto bytes = [](int T, int G) { return 4 * std::max(tree_floats(T, D, G), cache_floats(TT, D, G)); };
+    cudaError_t e = allow_smem(tree_simt_kernel<ST, D, TT>, bytes(TT, D / 32));
+    if (e != cudaSuccess) return e;
+    tree_simt_kernel<ST, D, TT><<<BH * (a.parts + 1), kThreads, bytes(a.T, a.G), st>>>(a);
+    count_launch();
+    return cudaGetLastError();
+}
+template <typename ST, int D>
+cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
+    if (a.T <= 4) return launch<ST, D, 4>(a, BH, st);
+    if (a.T <= 16) return launch<ST, D, 16>(a, BH, st);
+    return launch<ST, D, 64>(a, BH, st);
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(int B, int H, int T, int d) {
+    const size_t BH = (size_t)B * H;
+    return off_pairs(BH) + (BH * pair_floats(T, d, max_parts((int)BH)) * 4 + 255) / 256 * 256;
+}
+
+cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool tensor_cores, cudaStream_t st) {
+    const int BH = s.B * s.H;
+    Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
+           c.out, c.u, c.lse, (uint8_t *)c.ws, s.H, s.L, c.cap, hg.G, 0, 1, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
+    a.parts = std::min(max_parts(BH), (c.cap + kTileKeys - 1) / kTileKeys);
+    if (s.bf16) return s.d == 128 ? by_rows<__nv_bfloat16, 128>(a, BH, st) : by_rows<__nv_bfloat16, 64>(a, BH, st);
+    return s.d == 128 ? by_rows<float, 128>(a, BH, st) : by_rows<float, 64>(a, BH, st);
+}
+
+}  // namespace natsl
