@@ -182,4 +182,8 @@ __device__ __forceinline__ void join_pair(const Args &a, int b, int h, int n) {
 }
 
 }  // namespace tree
+
+// tree_tc.cu: bf16 storage, one or two softmax heads per linear head
+cudaError_t launch_tree_tc(const tree::Args &a, int BH, int d, cudaStream_t st);
+
 }  // namespace natsl

@@ -308,6 +308,7 @@ cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool ten
     Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
            c.out, c.u, c.lse, (uint8_t *)c.ws, s.H, s.L, c.cap, hg.G, 0, 1, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
     a.parts = std::min(max_parts(BH), (c.cap + kTileKeys - 1) / kTileKeys);
+    if (tensor_cores && hg.G <= 2) return launch_tree_tc(a, BH, s.d, st);
     if (s.bf16) return s.d == 128 ? by_rows<__nv_bfloat16, 128>(a, BH, st) : by_rows<__nv_bfloat16, 64>(a, BH, st);
     return s.d == 128 ? by_rows<float, 128>(a, BH, st) : by_rows<float, 64>(a, BH, st);
 }
