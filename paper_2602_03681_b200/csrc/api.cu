@@ -447,7 +447,7 @@ int natsl_workspace_size(const natsl_params *p, int op, size_t *bytes) {
     switch (op) {
         case NATSL_OP_TREE:
             if (p->L < 1 || p->L > kTreeNodes) return NATSL_ERR_SHAPE;
-            *bytes = tree_workspace_bytes(p->B, p->H, p->L, p->d);
+            *bytes = tree_workspace_bytes();
             return NATSL_OK;
         case NATSL_OP_FWD: *bytes = carve_fwd(p, nullptr).bytes; return NATSL_OK;
         case NATSL_OP_BWD: *bytes = carve_bwd(p, nullptr).bytes; return NATSL_OK;
@@ -860,7 +860,7 @@ int natsl_tree_step(const void *q, const void *k, const void *v, const float *g,
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(u) || !aligned16(state) ||
         !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(ws))
         return NATSL_ERR_ALIGN;
-    if (!ws || ws_bytes < tree_workspace_bytes(p->B, p->H, p->L, p->d)) return NATSL_ERR_WORKSPACE;
+    if (!ws || ws_bytes < tree_workspace_bytes()) return NATSL_ERR_WORKSPACE;
     const TreeCall c{q, k, v, g, beta, route, parent, n_nodes, p->w, state, k_cache, v_cache, cache_len, cache_cap,
                      out, u, p->lse, p->scale_la, p->scale_sm, p->eps, ws};
     cudaError_t e = launch_tree_step(c, shape_of(p), head_groups(p), use_tensor_cores(p), static_cast<cudaStream_t>(stream));
@@ -879,7 +879,7 @@ int natsl_tree_commit(const void *k, const void *v, const float *g, const uint8_
     if (!aligned16(k) || !aligned16(v) || !aligned16(u) || !aligned16(state) || !aligned16(k_cache) ||
         !aligned16(v_cache) || !aligned16(ws))
         return NATSL_ERR_ALIGN;
-    if (!ws || ws_bytes < tree_workspace_bytes(p->B, p->H, p->L, p->d)) return NATSL_ERR_WORKSPACE;
+    if (!ws || ws_bytes < tree_workspace_bytes()) return NATSL_ERR_WORKSPACE;
     cudaError_t e = launch_tree_commit(k, v, g, route, u, path, n_path, state, k_cache, v_cache, cache_len, cache_cap,
                                        shape_of(p), head_groups(p).norm_eps, ws, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? NATSL_OK : NATSL_ERR_CUDA;

@@ -358,9 +358,7 @@ struct TreeCall {
     float scale_la, scale_sm, eps;
     void *ws;
 };
-// Status word, per-pair tickets, linear read-outs, partial results.  Zero-filled once by the caller; the kernels leave the
-// tickets at zero.
-size_t tree_workspace_bytes(int B, int H, int T, int d);
+size_t tree_workspace_bytes();                    // the status word's page
 cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool tensor_cores, cudaStream_t st);
 // tree_commit.cu
 cudaError_t launch_tree_commit(const void *k, const void *v, const float *g, const uint8_t *route, const float *u,

@@ -1,5 +1,12 @@
 // What the two tree-step kernels (tensor cores, fp32 CUDA cores) share: how a pair's work is cut, the walk up the drafted
 // tree, and the join of the partial results.
+//
+// A (sequence, head) pair is the work of one cluster of 2, 4 or 8 CTAs.  Each takes a slice of the retained K/V for all nodes,
+// and d / cluster columns of the tree's own part (linear branch, and the softmax over the tree's own tokens).  The partial
+// results stay in shared memory; behind the cluster's barrier each CTA joins every cluster-th row of the tree, reading its
+// neighbours' shares over distributed shared memory.  So a call is one launch, needs no scratch and no atomics, and the sums
+// have the same order on every call.  (With partial results in global memory and the last of a pair's CTAs, by a ticket,
+// joining them alone, 16 nodes of 16 pairs took 44 us, 25 of them in that join.)
 #pragma once
 #include "common.cuh"
 #include "natsl_internal.h"
@@ -10,30 +17,8 @@ namespace tree {
 
 constexpr int kMaxNodes = 64;        // one machine word of ancestors per node
 constexpr int kThreads = 128;
-constexpr int kTileKeys = 64;        // keys the cut of a cache is counted in
+constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// Cache items per (sequence, head) that the workspace has room for, by the number of pairs alone.
-__host__ __device__ inline int max_parts(int BH) {
-    const int p = 592 / BH;
-    return p < 4 ? 4 : (p > 64 ? 64 : p);
-}
-// Workspace: [0,256) status word; tickets [BH] i32; per pair the linear read-outs [T][D], then parts + 1 partial results
-// (the last one is the tree's own): m [4][T] in base-2 units, z [4][T], acc [T][D].
-__host__ __device__ inline size_t off_pairs(size_t BH) { return (256 + BH * 4 + 255) / 256 * 256; }
-__host__ __device__ inline size_t part_floats(int T, int D) { return (size_t)T * (8 + D); }
-__host__ __device__ inline size_t pair_floats(int T, int D, int parts) { return (size_t)T * D + (parts + 1) * part_floats(T, D); }
-
-// A stored length outside [0, cap] counts as the nearer of both.  Of `parts` items the first np take tpp tiles each.
-struct Cut { int n, tpp, np; };
-__device__ __forceinline__ Cut cut_of(int n_raw, int cap, int parts, int least_tiles) {
-    Cut c;
-    c.n = min(max(n_raw, 0), cap);
-    const int tiles = (c.n + kTileKeys - 1) / kTileKeys;
-    c.tpp = max(least_tiles, (tiles + parts - 1) / parts);
-    c.np = (tiles + c.tpp - 1) / c.tpp;
-    return c;
-}
 
 struct Args {
     const void *q, *k, *v;
@@ -45,12 +30,23 @@ struct Args {
     const int32_t *cache_len;
     void *out;
     float *u, *lse;
-    uint8_t *ws;
-    int H, T, cap, G, parts, least_tiles;
+    int32_t *status;
+    int H, T, cap, G, cluster;
     float scale_la, scale_sm, eps, norm_eps;      // norm_eps < 0: q, k as given
 };
 
-// Shared-memory head of a CTA: the tree.
+// A cache's share of CTA `rank`: keys [from, to).  A stored length outside [0, cap] counts as the nearer of both.
+struct Share { int from, to; };
+__device__ __forceinline__ Share share_of(int n_raw, int cap, int cluster, int rank) {
+    const int n = min(max(n_raw, 0), cap), blocks = n / 16 + (n % 16 != 0), per = (blocks + cluster - 1) / cluster;
+    const int from = (int)min((long long)rank * per * 16, (long long)n);
+    return Share{from, (int)min((long long)from + (long long)per * 16, (long long)n)};
+}
+
+// Head of a CTA's dynamic shared memory, read by the whole cluster: running maxima (base 2) and sums of the CTA's cache share,
+// and those of the softmax over the tree's own tokens for the softmax heads of the CTA's columns.
+struct Sums { float cache_m[4][kMaxNodes], cache_z[4][kMaxNodes], tree_m[4][kMaxNodes], tree_z[4][kMaxNodes]; };
+
 struct Nodes {
     unsigned long long above[kMaxNodes];          // strict ancestors
     unsigned long long fold, keep;                // nodes that update the state; nodes whose K/V count as retained
@@ -71,7 +67,6 @@ __device__ __forceinline__ int nodes_of(const Args &a, int b) {
 // products along the path, so that a decay of zero (g = -inf) stays zero and long paths lose nothing by cancellation.
 __device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, Nodes *nd, float *decay, int pitch) {
     const int tid = threadIdx.x;
-    int32_t *status = reinterpret_cast<int32_t *>(a.ws);
     if (tid < kMaxNodes) {
         int par = -1, rv = 0;
         if (tid < n) {
@@ -79,7 +74,7 @@ __device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, N
             par = a.parent[(size_t)b * a.T + tid];
             if (par < -1 || par >= tid) {         // not a tree: reported, and taken as a child of the context
                 par = -1;
-                atomicMin(status, (int)NATSL_ERR_TREE);
+                atomicMin(a.status, (int)NATSL_ERR_TREE);
             }
             rv = a.route[at];
             nd->beta[tid] = a.beta[at];
@@ -93,9 +88,9 @@ __device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, N
         }
     }
     if (tid == 0) {
-        if (a.n_nodes && a.n_nodes[b] != n) atomicMin(status, (int)NATSL_ERR_TREE);
+        if (a.n_nodes && a.n_nodes[b] != n) atomicMin(a.status, (int)NATSL_ERR_TREE);
         const int len = a.cache_len[(size_t)b * a.H + h];
-        if (len < 0 || len > a.cap) atomicMin(status, (int)NATSL_ERR_CACHE_FULL);
+        if (len < 0 || len > a.cap) atomicMin(a.status, (int)NATSL_ERR_CACHE_FULL);
     }
     __syncthreads();
     if (tid < n) {
@@ -112,73 +107,116 @@ __device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, N
     } else if (tid < kMaxNodes) {
         nd->above[tid] = 0;
         nd->whole[tid] = 0.f;
+        nd->beta[tid] = 0.f;
     }
 }
 
-// Pair bh is finished by whichever of its parts + 1 items comes last (an atomic ticket, nobody waits); true in that CTA.
-__device__ __forceinline__ bool last_of_pair(const Args &a, int bh) {
-    __shared__ int s_last;
-    __syncthreads();                              // every thread's partial results are written
-    if (threadIdx.x == 0) {
-        int32_t *ticket = reinterpret_cast<int32_t *>(a.ws + 256) + bh;
-        __threadfence();
-        const int last = tc::atom_add_acq_rel(ticket, 1) == a.parts;
-        if (last) *ticket = 0;                    // ready for the next call
-        __threadfence();
-        s_last = last;
-    }
-    __syncthreads();
-    return s_last != 0;
+// The cluster's barrier: what its threads have written to shared memory is there for all of them.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// `p`'s counterpart in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote(const void *p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(tc::smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_remote(uint32_t p) {
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(p) : "memory");
+    return x;
+}
+template <int V> __device__ __forceinline__ void ld_remote(uint32_t p, float (&x)[V]) {
+    if constexpr (V == 4)
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(p) : "memory");
+    else
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(p) : "memory");
 }
 
-// Joins the partial results of pair (b, h): softmax over cache items and the tree, both branches normalised and combined.
-// A warp takes a row; lane l owns columns V l .. V l + V - 1.
+// Joins the rows rank, rank + cluster, ... of pair (b, h): softmax over the cache shares and the tree, both branches normalised
+// and combined.  A warp takes a row; lane l owns columns V l .. V l + V - 1.  acc [rows][acc_pitch]: the CTA's sums over its
+// cache share, all columns; o_la, o_tree [rows][D / cluster]: the linear read-out and the sums over the tree, its own columns.
 template <typename ST, int D>
-__device__ __forceinline__ void join_pair(const Args &a, int b, int h, int n) {
+__device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, int rank, const Sums *sums, const float *acc, int acc_pitch,
+                                          const float *o_la, const float *o_tree) {
     constexpr int V = D / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int bh = b * a.H + h, G = a.G, ls = 32 / G, sg = lane / ls;
-    const Cut c = cut_of(a.cache_len[bh], a.cap, a.parts, a.least_tiles);
-    const float *base = reinterpret_cast<const float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
-                        (size_t)bh * pair_floats(a.T, D, a.parts);
-    const size_t pf = part_floats(a.T, D);
-    const float *first = base + (size_t)a.T * D, *own = first + a.parts * pf;
-    for (int t = warp; t < n; t += kThreads / 32) {
-        float M = __ldcg(own + sg * a.T + t), Z = 0.f, o[V], ol[V];
-        for (int p = 0; p < c.np; ++p) M = fmaxf(M, __ldcg(first + p * pf + sg * a.T + t));
-        const float Mu = M == -INFINITY ? 0.f : M;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.G, ls = 32 / G, sg = lane / ls, cols = D / a.cluster;
+    const int owner = lane * V / cols, at = lane * V - owner * cols;
+    cluster_sync();
+    for (int t = rank + a.cluster * warp; t < n; t += a.cluster * (kThreads / 32)) {
+        const size_t row = ((size_t)b * a.T + t) * a.H + h;
+        const float wn = a.w ? a.w[row * 2] : 0.5f, wl = a.w ? a.w[row * 2 + 1] : 0.5f;
+        float m[kMaxCluster], z[kMaxCluster], x[kMaxCluster][V], o[V], ol[V];
 #pragma unroll
-        for (int x = 0; x < V; ++x) {
-            o[x] = 0.f;
-            ol[x] = __ldcg(base + (size_t)t * D + lane * V + x);
+        for (int r = 0; r < kMaxCluster; ++r) {
+            m[r] = -INFINITY;
+            if (r < a.cluster) {
+                m[r] = ld_remote(remote(&sums->cache_m[sg][t], r));
+                z[r] = ld_remote(remote(&sums->cache_z[sg][t], r));
+                ld_remote<V>(remote(acc + t * acc_pitch + lane * V, r), x[r]);
+            }
         }
-        for (int p = 0; p <= c.np; ++p) {         // (in this order whoever joins: the same sums on every call)
-            const float *pp = p < c.np ? first + p * pf : own;
-            const float f = tc::ex2_ftz(__ldcg(pp + sg * a.T + t) - Mu);
-            Z = fmaf(__ldcg(pp + (4 + sg) * a.T + t), f, Z);
-            const float *acc = pp + 8 * a.T + (size_t)t * D + lane * V;
+        const float mt = ld_remote(remote(&sums->tree_m[sg][t], owner)), zt = ld_remote(remote(&sums->tree_z[sg][t], owner));
+        ld_remote<V>(remote(o_tree + t * cols + at, owner), o);
+        ld_remote<V>(remote(o_la + t * cols + at, owner), ol);
+        float M = mt;
 #pragma unroll
-            for (int x = 0; x < V; ++x) o[x] = fmaf(__ldcg(acc + x), f, o[x]);
-        }
+        for (int r = 0; r < kMaxCluster; ++r) M = fmaxf(M, m[r]);
+        const float Mu = M == -INFINITY ? 0.f : M, ft = tc::ex2_ftz(mt - Mu);
+        float Z = zt * ft;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] *= ft;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r)
+            if (r < a.cluster) {
+                const float f = tc::ex2_ftz(m[r] - Mu);
+                Z = fmaf(z[r], f, Z);
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = fmaf(x[r][i], f, o[i]);
+            }
         const float iz = Z == 0.f ? 0.f : 1.f / Z;     // (no visible key: o_nla = 0)
         float sn = 0.f, sl = 0.f;
 #pragma unroll
-        for (int x = 0; x < V; ++x) {
-            o[x] *= iz;
-            sn = fmaf(o[x], o[x], sn);
-            sl = fmaf(ol[x], ol[x], sl);
+        for (int i = 0; i < V; ++i) {
+            o[i] *= iz;
+            sn = fmaf(o[i], o[i], sn);
+            sl = fmaf(ol[i], ol[i], sl);
         }
         for (int s = ls / 2; s > 0; s >>= 1) sn += __shfl_xor_sync(0xffffffffu, sn, s);
         sl = warp_sum(sl);
-        const size_t row = ((size_t)b * a.T + t) * a.H + h;
-        const float wn = a.w ? a.w[row * 2] : 0.5f, wl = a.w ? a.w[row * 2 + 1] : 0.5f;
         const float fn = wn * rsqrtf(sn / (D / G) + a.eps), fl = wl * rsqrtf(sl / D + a.eps);
         ST *out = reinterpret_cast<ST *>(a.out) + row * D + lane * V;
+        float y[V];
 #pragma unroll
-        for (int x = 0; x < V; ++x) out[x] = from_f32<ST>(fn * o[x] + fl * ol[x]);
+        for (int i = 0; i < V; ++i) y[i] = fmaf(fn, o[i], fl * ol[i]);
+        if constexpr (V == 4) {
+            store4(out, make_float4(y[0], y[1], y[2], y[3]));
+        } else {
+            out[0] = from_f32<ST>(y[0]);
+            out[1] = from_f32<ST>(y[1]);
+        }
         if (a.lse && lane % ls == 0)
-            a.lse[((size_t)bh * G + sg) * a.T + t] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * kLn2;
+            a.lse[(((size_t)b * a.H + h) * G + sg) * a.T + t] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * kLn2;
     }
+    cluster_sync();                               // nobody's shared memory goes while a neighbour still reads it
+}
+
+// One cluster per pair.
+template <typename K> cudaError_t launch_clusters(K kernel, const Args &a, int BH, size_t smem, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(BH * a.cluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    count_launch();
+    return e;
 }
 
 }  // namespace tree

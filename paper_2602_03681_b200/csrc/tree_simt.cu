@@ -8,8 +8,7 @@
 // so the state is read once and never written, and the tokens' own products form two T x T tables.  Sums over ancestors
 // run over the set bits of the node's ancestor word: a sibling's infinity or NaN cannot reach a node through 0 * inf.
 //
-// A pair's work is cut into cache items (slices of the retained K/V) and one tree item (linear branch, the tree's own
-// part of the softmax); the last of them to finish joins the partial results.  Bound by the fp32 pipes.
+// Bound by the fp32 pipes; tree_common.cuh has the cut into CTAs and the join.
 #include <algorithm>
 #include "tree_common.cuh"
 
@@ -21,15 +20,21 @@ using namespace tree;
 constexpr int kKeys = 32;                         // keys per tile: one per lane
 constexpr int kWarps = kThreads / 32;
 
-__host__ __device__ inline int tree_floats(int T, int D, int G) { return 2 * T * (D + 4) + T * D + (2 + G) * T * T; }
+constexpr int kHead = sizeof(Sums) / 4;           // floats; then acc [T][D + 4], then what one of the two parts needs:
+__host__ __device__ inline int acc_floats(int T, int D) { return T * (D + 4); }
+// the tree's part: o_la, o_tree, u (own columns); q, k; two tables and the probabilities of the columns' softmax heads
+__host__ __device__ inline int tree_floats(int T, int D, int G, int cluster) {
+    const int cols = D / cluster, heads = cols * G > D ? cols * G / D : 1;
+    return 3 * T * cols + 2 * T * (D + 4) + (2 + heads) * T * T;
+}
 __host__ __device__ inline int cache_floats(int TT, int D, int G) {
     return TT * (D + 4) + kKeys * (D + 4) + kKeys * D + G * TT * kKeys + 3 * G * TT + G * kKeys;
 }
 
-// One cache item.  Lane = key for the logits (a warp owns whole rows of a tile, so maximum and sum are shuffles), thread =
+// The CTA's share of the cache.  Lane = key for the logits (a warp owns whole rows of a tile, so maximum and sum are shuffles), thread =
 // column for the products with V (RC rows of accumulators).
 template <typename ST, int D, int TT>
-__device__ void cache_item(const Args &a, float *sm, int b, int h, int part, int n_nodes, const Cut &c) {
+__device__ void cache_part(const Args &a, Sums *sums, float *out_acc, float *sm, int b, int h, int n_nodes, const Share &c) {
     constexpr int RC = TT * D / 128, P = D + 4;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G;
     const int bh = b * a.H + h;
@@ -57,8 +62,8 @@ __device__ void cache_item(const Args &a, float *sm, int b, int h, int part, int
     for (int r = 0; r < RC; ++r) acc[r] = 0.f;
     const ST *kc = reinterpret_cast<const ST *>(a.k_cache) + (size_t)bh * a.cap * D;
     const ST *vc = reinterpret_cast<const ST *>(a.v_cache) + (size_t)bh * a.cap * D;
-    const int from = part * c.tpp * kTileKeys, to = min(c.n, from + c.tpp * kTileKeys);
-    for (int j0 = from; j0 < to; j0 += kKeys) {
+    const int to = c.to;
+    for (int j0 = c.from; j0 < to; j0 += kKeys) {
         __syncthreads();                          // (the tile before has been read)
         for (int i = tid; i < kKeys * D / 4; i += kThreads) {
             const int j = i / (D / 4), x = (i - j * (D / 4)) * 4;
@@ -121,25 +126,25 @@ __device__ void cache_item(const Args &a, float *sm, int b, int h, int part, int
         }
     }
     __syncthreads();
-    float *pp = reinterpret_cast<float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
-                (size_t)bh * pair_floats(a.T, D, a.parts) + (size_t)a.T * D + part * part_floats(a.T, D);
     for (int i = tid; i < G * TT; i += kThreads) {
         const int g = i / TT, t = i - g * TT;
-        if (t < n_nodes) { pp[g * a.T + t] = s_m[i]; pp[(4 + g) * a.T + t] = s_z[i]; }
+        sums->cache_m[g][t] = s_m[i];
+        sums->cache_z[g][t] = s_z[i];
     }
 #pragma unroll
     for (int r = 0; r < RC; ++r)
-        if (r0 + r < n_nodes) pp[8 * a.T + (size_t)(r0 + r) * D + col] = acc[r];
+        if (r0 + r < n_nodes) out_acc[(r0 + r) * P + col] = acc[r];
 }
 
-// The tree item: linear branch and the tree's own part of the softmax.
+// The tree's own part, for the columns c0 .. c0 + D / cluster - 1.
 template <typename ST, int D>
-__device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int n) {
+__device__ void tree_part(const Args &a, Sums *sums, float *sm, Nodes *nd, int b, int h, int n, int rank) {
     constexpr int P = D + 4;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G, T = a.T;
-    const int bh = b * a.H + h;
-    float *sq = sm, *sk = sq + T * P, *su = sk + T * P, *sa = su + T * D, *sb = sa + T * T, *sp = sb + T * T;
-    const ST *v = reinterpret_cast<const ST *>(a.v) + ((size_t)b * T * a.H + h) * D;      // row t: v + t H D
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G, T = a.T, cols = D / a.cluster, c0 = rank * cols;
+    const int g0 = c0 / ds, heads = (c0 + cols - 1) / ds - g0 + 1;       // softmax heads that these columns belong to
+    float *so = sm, *st = so + T * cols, *su = st + T * cols, *sq = su + T * cols, *sk = sq + T * P, *sa = sk + T * P, *sb = sa + T * T,
+          *sp = sb + T * T;
+    const ST *v = reinterpret_cast<const ST *>(a.v) + ((size_t)b * T * a.H + h) * D + c0;      // row t: v + t H D
     for (int i = tid; i < n * D; i += kThreads) {
         const int t = i / D, x = i - t * D;
         const size_t at = (((size_t)b * T + t) * a.H + h) * D + x;
@@ -176,19 +181,18 @@ __device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int
         }
     }
     __syncthreads();
-    // k S0 and q S0: thread = column, eight rows at a time; d = 64: two threads share a column, every other group of rows
-    float *base = reinterpret_cast<float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
-                  (size_t)bh * pair_floats(T, D, a.parts);
-    const int col = tid % D, side = tid / D;
-    const float *S = a.state + (size_t)bh * D * D + col;
-    for (int t0 = side * 8; t0 < n; t0 += 8 * kThreads / D) {
-        float ak[8], aq[8];
+    // k S0 and q S0: thread = column and a group of rows, four rows at a time
+    const int col = tid % cols, side = tid / cols, sides = kThreads / cols;
+    const float *S = a.state + ((size_t)b * a.H + h) * D * D + c0 + col;
+    for (int t0 = side * 4; t0 < n; t0 += 4 * sides) {
+        float ak[4], aq[4];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) ak[r] = aq[r] = 0.f;
+        for (int r = 0; r < 4; ++r) ak[r] = aq[r] = 0.f;
+#pragma unroll 4
         for (int x = 0; x < D; x += 4) {
             const float s0 = S[(size_t)x * D], s1 = S[(size_t)(x + 1) * D], s2 = S[(size_t)(x + 2) * D], s3 = S[(size_t)(x + 3) * D];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
+            for (int r = 0; r < 4; ++r) {
                 const int t = min(t0 + r, n - 1);
                 const float4 kk = *reinterpret_cast<const float4 *>(sk + t * P + x), qq = *reinterpret_cast<const float4 *>(sq + t * P + x);
                 ak[r] = fmaf(kk.x, s0, fmaf(kk.y, s1, fmaf(kk.z, s2, fmaf(kk.w, s3, ak[r]))));
@@ -196,11 +200,11 @@ __device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int
             }
         }
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < 4; ++r) {
             const int t = t0 + r;
             if (t >= n) break;
-            su[t * D + col] = nd->beta[t] * (to_f32(v[(size_t)t * a.H * D + col]) - nd->whole[t] * nd->rk_la[t] * ak[r]);
-            base[(size_t)t * D + col] = a.scale_la * nd->whole[t] * nd->rq_la[t] * aq[r];
+            su[t * cols + col] = nd->beta[t] * (to_f32(v[(size_t)t * a.H * D + col]) - nd->whole[t] * nd->rk_la[t] * ak[r]);
+            so[t * cols + col] = a.scale_la * nd->whole[t] * nd->rq_la[t] * aq[r];
         }
     }
     // the tables, where j is above i or i itself (sb holds the decays)
@@ -216,7 +220,7 @@ __device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int
                 qg = fmaf(q4.x, y.x, fmaf(q4.y, y.y, fmaf(q4.z, y.z, fmaf(q4.w, y.w, qg))));
                 kk = fmaf(k4.x, y.x, fmaf(k4.y, y.y, fmaf(k4.z, y.z, fmaf(k4.w, y.w, kk))));
             }
-            sp[(g * T + t) * T + j] = a.scale_sm * kLog2e * nd->rq_sm[g][t] * nd->rk_sm[g][j] * qg;
+            if (g >= g0 && g < g0 + heads) sp[((g - g0) * T + t) * T + j] = a.scale_sm * kLog2e * nd->rq_sm[g][t] * nd->rk_sm[g][j] * qg;
             qk += qg;
         }
         const float dec = sb[t * T + j];
@@ -224,8 +228,7 @@ __device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int
         sb[t * T + j] = a.scale_la * dec * nd->rq_la[t] * nd->rk_la[j] * qk;
     }
     __syncthreads();
-    float *own = base + (size_t)T * D + a.parts * part_floats(T, D);
-    for (int i = tid; i < G * n; i += kThreads) {  // the softmax over the kept nodes of the path
+    for (int i = tid; i < heads * n; i += kThreads) {  // the softmax over the kept nodes of the path
         const int g = i / n, t = i - g * n;
         float m = -INFINITY, z = 0.f;
         const unsigned long long seen = (nd->above[t] | 1ull << t) & nd->keep;
@@ -236,19 +239,19 @@ __device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int
             const int j = __ffsll(w) - 1;
             z += row[j] = tc::ex2_ftz(row[j] - mu);
         }
-        own[g * T + t] = m;
-        own[(4 + g) * T + t] = z;
+        sums->tree_m[g0 + g][t] = m;
+        sums->tree_z[g0 + g][t] = z;
     }
     __syncthreads();
     // up the tree node by node; a column's thread needs no other column
-    if (tid < D) {
-        const int gc = col / ds;
+    if (tid < cols) {
+        const int gc = (c0 + col) / ds - g0;
         for (int t = 0; t < n; ++t) {
-            float u = su[t * D + col], o = base[(size_t)t * D + col], s = 0.f;
+            float u = su[t * cols + col], o = so[t * cols + col], s = 0.f;
             for (unsigned long long w = nd->above[t]; w; w &= w - 1) {
                 const int j = __ffsll(w) - 1;
                 if (nd->fold >> j & 1) {
-                    const float x = su[j * D + col];
+                    const float x = su[j * cols + col];
                     u = fmaf(-sa[t * T + j], x, u);
                     o = fmaf(sb[t * T + j], x, o);
                 }
@@ -257,10 +260,10 @@ __device__ void tree_item(const Args &a, float *sm, Nodes *nd, int b, int h, int
             if (nd->fold >> t & 1) o = fmaf(sb[t * T + t], u, o);
             else u = 0.f;
             if (nd->keep >> t & 1) s = fmaf(sp[(gc * T + t) * T + t], to_f32(v[(size_t)t * a.H * D + col]), s);
-            su[t * D + col] = u;
-            base[(size_t)t * D + col] = o;
-            own[8 * T + (size_t)t * D + col] = s;
-            if (a.u) a.u[(((size_t)b * T + t) * a.H + h) * D + col] = u;
+            su[t * cols + col] = u;
+            so[t * cols + col] = o;
+            st[t * cols + col] = s;
+            if (a.u) a.u[(((size_t)b * T + t) * a.H + h) * D + c0 + col] = u;
         }
     }
 }
@@ -269,25 +272,23 @@ template <typename ST, int D, int TT>
 __global__ void __launch_bounds__(kThreads) tree_simt_kernel(Args a) {
     extern __shared__ __align__(16) float dyn[];
     __shared__ Nodes nodes;
-    const int per_pair = a.parts + 1, bh = blockIdx.x / per_pair, part = blockIdx.x - bh * per_pair - 1;   // part -1: the tree
-    const int b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
-    if (part < 0) {
-        tree_item<ST, D>(a, dyn, &nodes, b, h, n);
-    } else {
-        const Cut c = cut_of(a.cache_len[bh], a.cap, a.parts, a.least_tiles);
-        if (part < c.np) cache_item<ST, D, TT>(a, dyn, b, h, part, n, c);
-    }
-    if (last_of_pair(a, bh)) join_pair<ST, D>(a, b, h, n);
+    const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
+    Sums *sums = reinterpret_cast<Sums *>(dyn);
+    float *acc = dyn + kHead, *work = acc + acc_floats(a.T, D);
+    cache_part<ST, D, TT>(a, sums, acc, work, b, h, n, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
+    __syncthreads();
+    tree_part<ST, D>(a, sums, work, &nodes, b, h, n, rank);
+    join_rows<ST, D>(a, b, h, n, rank, sums, acc, D + 4, work, work + a.T * (D / a.cluster));
 }
 
 template <typename ST, int D, int TT>
 cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
-    const auto bytes = [](int T, int G) { return 4 * std::max(tree_floats(T, D, G), cache_floats(TT, D, G)); };
-    cudaError_t e = allow_smem(tree_simt_kernel<ST, D, TT>, bytes(TT, D / 32));
+    const auto bytes = [](int T, int G, int cluster) {
+        return 4 * (kHead + acc_floats(T, D) + std::max(tree_floats(T, D, G, cluster), cache_floats(TT, D, G)));
+    };
+    cudaError_t e = allow_smem(tree_simt_kernel<ST, D, TT>, bytes(TT, D / 32, 2));
     if (e != cudaSuccess) return e;
-    tree_simt_kernel<ST, D, TT><<<BH * (a.parts + 1), kThreads, bytes(a.T, a.G), st>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    return launch_clusters(tree_simt_kernel<ST, D, TT>, a, BH, bytes(a.T, a.G, a.cluster), st);
 }
 template <typename ST, int D>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
@@ -298,16 +299,14 @@ cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
 
 }  // namespace
 
-size_t tree_workspace_bytes(int B, int H, int T, int d) {
-    const size_t BH = (size_t)B * H;
-    return off_pairs(BH) + (BH * pair_floats(T, d, max_parts((int)BH)) * 4 + 255) / 256 * 256;
-}
+size_t tree_workspace_bytes() { return 256; }
 
 cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool tensor_cores, cudaStream_t st) {
     const int BH = s.B * s.H;
-    Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
-           c.out, c.u, c.lse, (uint8_t *)c.ws, s.H, s.L, c.cap, hg.G, 0, 1, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
-    a.parts = std::min(max_parts(BH), (c.cap + kTileKeys - 1) / kTileKeys);
+    // CTAs per pair: as many as one resident set of two per multiprocessor has for each
+    const int cluster = BH * 8 <= 2 * 148 ? 8 : BH * 4 <= 2 * 148 ? 4 : 2;
+    const Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
+                 c.out, c.u, c.lse, (int32_t *)c.ws, s.H, s.L, c.cap, hg.G, cluster, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
     if (tensor_cores && hg.G <= 2) return launch_tree_tc(a, BH, s.d, st);
     if (s.bf16) return s.d == 128 ? by_rows<__nv_bfloat16, 128>(a, BH, st) : by_rows<__nv_bfloat16, 64>(a, BH, st);
     return s.d == 128 ? by_rows<float, 128>(a, BH, st) : by_rows<float, 64>(a, BH, st);

@@ -2,14 +2,18 @@
 // tree_simt.cu's; here the products are warp-level MMAs: a tree has 1 to 64 query rows, far below a tcgen05 tile of 128, and
 // the call is bound by reading the retained K/V once.
 //
-// Cache items stream K/V tiles of 64 keys through a ring of asynchronous copies.  The four warps share the tile by keys (and,
-// beyond 32 nodes, by two halves of the rows), each with its own running maximum and sum, so that a key's row leaves shared
-// memory once (twice) whatever the number of nodes; the warps' results meet at the end of the item.  A running maximum moves
-// only when a logit exceeds it by 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's own precision); their
-// sum is taken before the rounding.
+// The cache's share of a CTA streams in tiles of 64 keys through a ring of asynchronous copies.  The four warps share the tile
+// by keys (and, beyond 32 nodes, by two halves of the rows), each with its own running maximum and sum, so that a key's row
+// leaves shared memory once (twice) whatever the number of nodes; the warps' results meet at the end.  A running maximum
+// moves only when a logit exceeds it by 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's own precision);
+// their sum is taken before the rounding.
 //
-// The tree item multiplies q and k with the fp32 state as three bf16 terms that together hold all of its 24 bits, so that
-// u, which goes into the state at the commit, is as exact as on CUDA cores.
+// The tree's own part, for a CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32 state as three bf16 terms that
+// together hold all of its 24 bits, so that u, which goes into the state at the commit, is as exact as on CUDA cores; the
+// substitution for u in fp32, a thread per column, by blocks of 16 nodes without a look at the tree's shape (the table is
+// zero off the path); the read-outs as MMAs again, u and the table as two bf16 terms each (2^-16).  Zeros in the place of
+// what a node does not see would let an infinity or a NaN through, so values that are not finite take a slower way that
+// looks at the paths.
 #include <algorithm>
 #include "tree_common.cuh"
 
@@ -17,6 +21,8 @@ namespace natsl {
 namespace {
 
 using namespace tree;
+
+constexpr int kTileKeys = 64;
 using tc::ldmatrix_x4;
 using tc::ldmatrix_x4_trans;
 
@@ -25,6 +31,10 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The first sixteen lanes give the rows: two 8x8 matrices, transposed.
+__device__ __forceinline__ void ldmatrix_x2_trans(uint32_t saddr, uint32_t (&r)[2]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(saddr) : "memory");
 }
 // 16 bytes global -> shared past the registers; `in` false: zeros.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool in) {
@@ -41,27 +51,30 @@ template <int D, int R> struct Layout {
     static constexpr int kRowGroups = R / kMt, kKeyGroups = 4 / kRowGroups, kWarpKeys = kTileKeys / kKeyGroups;
     static constexpr int kRowBytes = D * 2, kTileBytes = kTileKeys * kRowBytes;
     static constexpr int kStages = D == 128 ? 3 : 4;
-    static constexpr int kRing = kStages * 2 * kTileBytes;
     static constexpr int kAccPitch = D + 4;
-    static constexpr int kMerge = kKeyGroups * kRows * kAccPitch * 4;
-    // tree item
+    static constexpr int oAcc = sizeof(Sums);                // the CTA's sums over its share of the cache
+    static constexpr int oWork = oAcc + kRows * kAccPitch * 4;
+    // while the cache is read: the ring (16-byte pieces swizzled by row), then the key groups' results over it and over oAcc
+    static constexpr int oRing = sizeof(Sums), kRing = kStages * 2 * kTileBytes, kMerge = kKeyGroups * kRows * kAccPitch * 4;
+    // the tree's part: q, k (then, in their places, u and o_la of the CTA's columns), v, the table
+    static constexpr int kCols = D / 2;                      // columns of a CTA, at most
     static constexpr int kPitch = kRowBytes + 16;            // (an odd number of 16-byte pieces: eight rows, eight banks)
-    static constexpr int oV = 0, oQ = oV + kRows * kPitch, oK = oQ + kRows * kPitch;
-    static constexpr int oA = oQ, oP = oA + kRows * kRows * 4;   // over q and k, once their products are in registers
-    static constexpr int kTables = kRows * kRows * (4 + 2 * 2), kOperands = 2 * kRows * kPitch;   // (two softmax heads at most)
-    static constexpr int oB = oQ + (kTables > kOperands ? kTables : kOperands), oU = oB + kRows * kRows * 4;
-    static constexpr int kTree = oU + kRows * D * 4;
-    static constexpr int kTotal = kRing > kMerge ? (kRing > kTree ? kRing : kTree) : (kMerge > kTree ? kMerge : kTree);
+    static constexpr int kPitchV = kCols * 2 + 16;
+    static constexpr int oQ = oWork, oK = oQ + kRows * kPitch, oV = oK + kRows * kPitch, oTab = oV + kRows * kPitchV;
+    static constexpr int kTabBytes = kRows * (kRows > kCols ? kRows : kCols) * 4;    // (the sums over the tree's V take its place)
+    static constexpr int kTree = oTab + kTabBytes;
+    static constexpr int kStream = oRing + (kRing > kMerge ? kRing : kMerge);
+    static constexpr int kTotal = kTree > kStream ? kTree : kStream;
 };
 
 template <int D, int G, bool kNorm, int R>
-__device__ void cache_item(const Args &a, uint8_t *sm, int b, int h, int part, int n_nodes, const Cut &c) {
+__device__ void cache_part(const Args &a, Sums *sums, uint8_t *sm, int b, int h, int n_nodes, const Share &c) {
     using L = Layout<D, R>;
     constexpr int ds = D / G, kMt = L::kMt, kNt = L::kWarpKeys / 8, kKs = ds / 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
     const int rg = warp / L::kKeyGroups, kg = warp - rg * L::kKeyGroups, r0 = rg * 16 * kMt;
     const int bh = b * a.H + h;
-    const uint32_t ring = tc::smem_u32(sm);
+    const uint32_t ring = tc::smem_u32(sm + L::oRing);
 
     // copies: thread = 16-byte piece of every eighth (sixteenth) row of a tile
     constexpr int kPieces = L::kRowBytes / 16, kStep = kThreads / kPieces;
@@ -69,22 +82,22 @@ __device__ void cache_item(const Args &a, uint8_t *sm, int b, int h, int part, i
     const uint8_t *kc = reinterpret_cast<const uint8_t *>(a.k_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
     const uint8_t *vc = reinterpret_cast<const uint8_t *>(a.v_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
     const uint32_t dst0 = row0 * L::kRowBytes + ((piece ^ (row0 & 7)) << 4);
-    const int t_begin = part * c.tpp, t_end = min((c.n + kTileKeys - 1) / kTileKeys, t_begin + c.tpp);
+    const int tiles = (c.to - c.from + kTileKeys - 1) / kTileKeys;
     auto fetch = [&](int t) {
-        if (t < t_end) {
-            const uint32_t at = ring + (t - t_begin) % L::kStages * 2 * L::kTileBytes + dst0;
+        if (t < tiles) {
+            const uint32_t at = ring + t % L::kStages * 2 * L::kTileBytes + dst0;
 #pragma unroll
             for (int i = 0; i < kTileKeys / kStep; ++i) {
-                const int j = t * kTileKeys + row0 + i * kStep;
-                const bool in = j < c.n;          // rows past the end count as zeros: what lies there may be anything
-                const size_t off = (size_t)(in ? j : 0) * L::kRowBytes;
+                const int j = c.from + t * kTileKeys + row0 + i * kStep;
+                const bool in = j < c.to;         // rows past the end count as zeros: what lies there may be anything
+                const size_t off = (size_t)(in ? j : c.from) * L::kRowBytes;
                 cp_async16(at + i * kStep * L::kRowBytes, kc + off, in);
                 cp_async16(at + L::kTileBytes + i * kStep * L::kRowBytes, vc + off, in);
             }
         }
         cp_async_commit();
     };
-    for (int i = 0; i < L::kStages - 1; ++i) fetch(t_begin + i);
+    for (int i = 0; i < L::kStages - 1; ++i) fetch(i);
 
     // q as A fragments, and each row's factor to base-2 logits
     uint32_t qf[kMt][D / 16][4];
@@ -131,13 +144,13 @@ __device__ void cache_item(const Args &a, uint8_t *sm, int b, int h, int part, i
             for (int r = 0; r < 2; ++r) { mx[s][m][r] = -INFINITY; z[s][m][r] = 0.f; }
     }
     const int key0 = kg * L::kWarpKeys;
-    for (int t = t_begin; t < t_end; ++t) {
+    for (int t = 0; t < tiles; ++t) {
         cp_async_wait<L::kStages - 2>();
         __syncthreads();                          // tile t is there, and every warp is done with tile t - 1 ...
         fetch(t + L::kStages - 1);                // ... whose place this one takes
-        const int left = c.n - t * kTileKeys - key0;      // of the warp's keys
+        const int left = c.to - c.from - t * kTileKeys - key0;      // of the warp's keys
         if (left <= 0) continue;
-        const uint32_t kt = ring + (t - t_begin) % L::kStages * 2 * L::kTileBytes, vt = kt + L::kTileBytes;
+        const uint32_t kt = ring + t % L::kStages * 2 * L::kTileBytes, vt = kt + L::kTileBytes;
 #pragma unroll
         for (int s = 0; s < G; ++s) {
             float x[kMt][kNt][4], kk[kNt];
@@ -249,11 +262,11 @@ __device__ void cache_item(const Args &a, uint8_t *sm, int b, int h, int part, i
             }
         }
     }
-    // the key groups' results -> one partial result
+    // the key groups' results -> the CTA's
     __shared__ float s_m[G][L::kKeyGroups][L::kRows], s_z[G][L::kKeyGroups][L::kRows];
     cp_async_wait<0>();
     __syncthreads();
-    float *acc = reinterpret_cast<float *>(sm);
+    float *acc = reinterpret_cast<float *>(sm + L::oAcc);    // the first key group's place is the result's
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
 #pragma unroll
@@ -271,11 +284,9 @@ __device__ void cache_item(const Args &a, uint8_t *sm, int b, int h, int part, i
             }
         }
     __syncthreads();
-    float *pp = reinterpret_cast<float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
-                (size_t)bh * pair_floats(a.T, D, a.parts) + (size_t)a.T * D + part * part_floats(a.T, D);
     for (int i = tid; i < n_nodes * (D / 4); i += kThreads) {
         const int t = i / (D / 4), x = (i - t * (D / 4)) * 4, s = x / ds;
-        float M = -INFINITY, e[L::kKeyGroups];
+        float M = -INFINITY;
 #pragma unroll
         for (int k = 0; k < L::kKeyGroups; ++k) M = fmaxf(M, s_m[s][k][t]);
         const float mu = M == -INFINITY ? 0.f : M;
@@ -283,15 +294,16 @@ __device__ void cache_item(const Args &a, uint8_t *sm, int b, int h, int part, i
         float Z = 0.f;
 #pragma unroll
         for (int k = 0; k < L::kKeyGroups; ++k) {
-            e[k] = tc::ex2_ftz(s_m[s][k][t] - mu);
+            const float e = tc::ex2_ftz(s_m[s][k][t] - mu);
             const float4 w = *reinterpret_cast<const float4 *>(acc + (k * L::kRows + t) * L::kAccPitch + x);
-            Z = fmaf(s_z[s][k][t], e[k], Z);
-            y.x = fmaf(w.x, e[k], y.x); y.y = fmaf(w.y, e[k], y.y);
-            y.z = fmaf(w.z, e[k], y.z); y.w = fmaf(w.w, e[k], y.w);
+            Z = fmaf(s_z[s][k][t], e, Z);
+            y.x = fmaf(w.x, e, y.x); y.y = fmaf(w.y, e, y.y);
+            y.z = fmaf(w.z, e, y.z); y.w = fmaf(w.w, e, y.w);
         }
-        *reinterpret_cast<float4 *>(pp + 8 * a.T + (size_t)t * D + x) = y;
-        if (x % ds == 0) { pp[s * a.T + t] = M; pp[(4 + s) * a.T + t] = Z; }
+        *reinterpret_cast<float4 *>(acc + t * L::kAccPitch + x) = y;
+        if (x % ds == 0) { sums->cache_m[s][t] = M; sums->cache_z[s][t] = Z; }
     }
+    __syncthreads();                              // (the other key groups' places are free)
 }
 
 // x as three bf16 terms, pairwise packed: what two rounded terms leave over is exact in the third.
@@ -305,28 +317,53 @@ __device__ __forceinline__ void split3(float x0, float x1, uint32_t (&t)[3]) {
     }
 }
 
+// ... and as two (2^-16 of x is left over).
+__device__ __forceinline__ void split2(float x0, float x1, uint32_t (&t)[2]) {
+    t[0] = tc::pack_bf162(x0, x1);
+    const float2 y = bf2(t[0]);
+    t[1] = tc::pack_bf162(x0 - y.x, x1 - y.y);
+}
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+__device__ __forceinline__ bool finite_bf16x2(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }
+
+// The tree's own part, for columns c0 .. c0 + cols - 1 (cols = D / cluster).
 template <int D, int G, bool kNorm, int R>
-__device__ void tree_item(const Args &a, uint8_t *sm, Nodes *nd, int b, int h, int n) {
+__device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int b, int h, int n, int rank) {
     using L = Layout<D, R>;
-    constexpr int ds = D / G, kRows = L::kRows, kCols = D / 4, kNs = kCols / 8;    // kCols: the state's columns per warp
+    constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
-    const int bh = b * a.H + h;
-    float *sa = reinterpret_cast<float *>(sm + L::oA), *sb = reinterpret_cast<float *>(sm + L::oB), *su = reinterpret_cast<float *>(sm + L::oU);
-    __half *sp = reinterpret_cast<__half *>(sm + L::oP);
-    float *base = reinterpret_cast<float *>(a.ws + off_pairs((size_t)gridDim.x / (a.parts + 1))) +
-                  (size_t)bh * pair_floats(T, D, a.parts);
-    float *own = base + (size_t)T * D + a.parts * part_floats(T, D);
+    const int bh = b * a.H + h, cols = D / a.cluster, c0 = rank * cols, sc = c0 / ds;   // sc: the columns' softmax head
+    float *tab = reinterpret_cast<float *>(sm + L::oTab);    // below the diagonal decays [i][j], above it [j][i]: what u_j takes from u_i
+    float *su = reinterpret_cast<float *>(sm + L::oQ), *so = reinterpret_cast<float *>(sm + L::oK), *st = tab;
+
+    // A tile of eight state columns as the B fragments of all products with it: rows 2 c4, + 1, + 8, + 9 of a step of 16.
+    const float *S = a.state + (size_t)bh * D * D + c0 + g4;
+    auto load = [&](int tile, float (&y)[kKs][4]) {
+#pragma unroll
+        for (int k = 0; k < kKs; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[k][i] = __ldg(S + (size_t)(16 * k + 2 * c4 + (i & 1) + (i >> 1) * 8) * D + tile * 8);
+    };
+    const int tiles = cols / 8;
+    float s[kKs][4];
+    if (warp < tiles) load(warp, s);
 
     constexpr int kPieces = L::kRowBytes / 16;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
     for (int i = tid; i < kRows * kPieces; i += kThreads) {
         const int t = i / kPieces, c = i - t * kPieces;
-        const size_t at = (((size_t)b * T + min(t, max(n - 1, 0))) * a.H + h) * kPieces + c;
-        const uint4 zero = make_uint4(0, 0, 0, 0);
+        const size_t at = (((size_t)b * T + min(t, n - 1)) * a.H + h) * kPieces + c;
         *reinterpret_cast<uint4 *>(sm + L::oQ + t * L::kPitch + c * 16) = t < n ? reinterpret_cast<const uint4 *>(a.q)[at] : zero;
         *reinterpret_cast<uint4 *>(sm + L::oK + t * L::kPitch + c * 16) = t < n ? reinterpret_cast<const uint4 *>(a.k)[at] : zero;
-        *reinterpret_cast<uint4 *>(sm + L::oV + t * L::kPitch + c * 16) = t < n ? reinterpret_cast<const uint4 *>(a.v)[at] : zero;
     }
-    read_nodes(a, b, h, n, nd, sb, kRows);
+    bool odd = false;                             // something that is not finite may meet a zero
+    for (int i = tid; i < kRows * tiles; i += kThreads) {
+        const int t = i / tiles, c = i - t * tiles;
+        const uint4 y = t < n ? reinterpret_cast<const uint4 *>(a.v)[(((size_t)b * T + t) * a.H + h) * kPieces + c0 / 8 + c] : zero;
+        odd |= !(finite_bf16x2(y.x) && finite_bf16x2(y.y) && finite_bf16x2(y.z) && finite_bf16x2(y.w));
+        *reinterpret_cast<uint4 *>(sm + L::oV + t * L::kPitchV + c * 16) = y;
+    }
+    read_nodes(a, b, h, n, nd, tab, kRows);
     __syncthreads();
     if (tid < 2 * kRows) {                        // a row's norms, thread = row of q or k
         const int t = tid % kRows;
@@ -334,92 +371,26 @@ __device__ void tree_item(const Args &a, uint8_t *sm, Nodes *nd, int b, int h, i
         const uint8_t *row = sm + (is_k ? L::oK : L::oQ) + t * L::kPitch;
         float all = 0.f;
 #pragma unroll
-        for (int s = 0; s < G; ++s) {
+        for (int g = 0; g < G; ++g) {
             float ss = 0.f;
             if (kNorm)
-                for (int c = s * kPieces / G; c < (s + 1) * kPieces / G; ++c) {
+                for (int c = g * kPieces / G; c < (g + 1) * kPieces / G; ++c) {
                     const uint4 y = *reinterpret_cast<const uint4 *>(row + c * 16);
                     const float2 y0 = bf2(y.x), y1 = bf2(y.y), y2 = bf2(y.z), y3 = bf2(y.w);
                     ss += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
                 }
-            (is_k ? nd->rk_sm : nd->rq_sm)[s][t] = kNorm ? rsqrtf(ss / ds + a.norm_eps) : 1.f;
+            (is_k ? nd->rk_sm : nd->rq_sm)[g][t] = kNorm ? rsqrtf(ss / ds + a.norm_eps) : 1.f;
             all += ss;
         }
         (is_k ? nd->rk_la : nd->rq_la)[t] = kNorm ? rsqrtf(all + a.norm_eps) : 1.f;
     }
     __syncthreads();
-    const uint32_t q_at = tc::smem_u32(sm + L::oQ), k_at = tc::smem_u32(sm + L::oK);
-    {
-        // k S0 and q S0.  A warp has kCols columns; the lane that holds column j of a B fragment loads kNs neighbouring columns,
-        // one for each of the warp's column tiles, so that a lane's results are 2 kNs neighbouring columns of a row.
-        float acc[2 * R][kNs][4];
-#pragma unroll
-        for (int m = 0; m < 2 * R; ++m)
-#pragma unroll
-            for (int i = 0; i < kNs; ++i)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) acc[m][i][x] = 0.f;
-        const float *S = a.state + (size_t)bh * D * D + warp * kCols + g4 * kNs;
-        float s[2][4][kNs];                       // rows 2 c4, + 1, + 8, + 9 of a step of 16
-        auto load = [&](int k, float (&y)[4][kNs]) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float *row = S + (size_t)(16 * k + 2 * c4 + (i & 1) + (i >> 1) * 8) * D;
-                if constexpr (kNs == 4) {
-                    const float4 v = __ldg(reinterpret_cast<const float4 *>(row));
-                    y[i][0] = v.x; y[i][1] = v.y; y[i][2] = v.z; y[i][3] = v.w;
-                } else {
-                    const float2 v = __ldg(reinterpret_cast<const float2 *>(row));
-                    y[i][0] = v.x; y[i][1] = v.y;
-                }
-            }
-        };
-        load(0, s[0]);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            if (k + 1 < D / 16) load(k + 1, s[(k + 1) & 1]);
-            uint32_t b0[kNs][3], b1[kNs][3];
-#pragma unroll
-            for (int i = 0; i < kNs; ++i) {
-                split3(s[k & 1][0][i], s[k & 1][1][i], b0[i]);
-                split3(s[k & 1][2][i], s[k & 1][3][i], b1[i]);
-            }
-#pragma unroll
-            for (int m = 0; m < 2 * R; ++m) {
-                uint32_t af[4];
-                ldmatrix_x4((m < R ? k_at : q_at) + ((m % R) * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af);
-#pragma unroll
-                for (int i = 0; i < kNs; ++i)
-#pragma unroll
-                    for (int x = 2; x >= 0; --x) mma_bf16(acc[m][i], af, b0[i][x], b1[i][x]);
-            }
-        }
-        const int col = warp * kCols + 2 * kNs * c4;
-#pragma unroll
-        for (int m = 0; m < 2 * R; ++m)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int t = (m % R) * 16 + r * 8 + g4;
-                const float fk = nd->whole[t] * nd->rk_la[t], fq = a.scale_la * nd->whole[t] * nd->rq_la[t], bt = nd->beta[t];
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int i = 0; i < kNs; i += 2) {
-                        const int at = col + x * kNs + i;
-                        if (m < R) {
-                            const float2 v = bf2(*reinterpret_cast<const uint32_t *>(sm + L::oV + t * L::kPitch + at * 2));
-                            *reinterpret_cast<float2 *>(su + t * D + at) =
-                                make_float2(bt * (v.x - fk * acc[m][i][2 * r + x]), bt * (v.y - fk * acc[m][i + 1][2 * r + x]));
-                        } else if (t < n) {
-                            *reinterpret_cast<float2 *>(base + (size_t)t * D + at) =
-                                make_float2(fq * acc[m][i][2 * r + x], fq * acc[m][i + 1][2 * r + x]);
-                        }
-                    }
-            }
-    }
-    {
-        // the tables: warp = 16 rows, all columns
-        constexpr int kNt = 2 * R;
+    const uint32_t q_at = tc::smem_u32(sm + L::oQ), k_at = tc::smem_u32(sm + L::oK), v_at = tc::smem_u32(sm + L::oV);
+
+    // ---- the tables: a warp has 16 rows, all columns.  What u takes from u goes to shared memory, what the read-out takes
+    // from u (two terms) and the probabilities stay in registers, as the A fragments of the read-out. ----
+    uint32_t bh_f[kNt / 2][4], bl_f[kNt / 2][4], p_f[kNt / 2][4];
+    if (warp < R) {
         float kk[kNt][4], qk[G][kNt][4];
 #pragma unroll
         for (int i = 0; i < kNt; ++i)
@@ -427,135 +398,280 @@ __device__ void tree_item(const Args &a, uint8_t *sm, Nodes *nd, int b, int h, i
             for (int x = 0; x < 4; ++x) {
                 kk[i][x] = 0.f;
 #pragma unroll
-                for (int s = 0; s < G; ++s) qk[s][i][x] = 0.f;
+                for (int g = 0; g < G; ++g) qk[g][i][x] = 0.f;
             }
-        if (warp < R) {
 #pragma unroll
-            for (int k = 0; k < D / 16; k += 2) {
-                uint32_t ak[2][4], aq[2][4];
+        for (int k = 0; k < kKs; k += 2) {
+            uint32_t ak[2][4], aq[2][4];
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const uint32_t off = (warp * 16 + (lane & 15)) * L::kPitch + (2 * (k + y) + (lane >> 4)) * 16;
-                    ldmatrix_x4(k_at + off, ak[y]);
-                    ldmatrix_x4(q_at + off, aq[y]);
-                }
+            for (int y = 0; y < 2; ++y) {
+                const uint32_t off = (warp * 16 + (lane & 15)) * L::kPitch + (2 * (k + y) + (lane >> 4)) * 16;
+                ldmatrix_x4(k_at + off, ak[y]);
+                ldmatrix_x4(q_at + off, aq[y]);
+            }
 #pragma unroll
-                for (int i = 0; i < kNt; ++i) {
-                    uint32_t bf[4];
-                    ldmatrix_x4(k_at + (i * 8 + (lane & 7)) * L::kPitch + (2 * k + (lane >> 3)) * 16, bf);
-                    mma_bf16(kk[i], ak[0], bf[0], bf[1]);
-                    mma_bf16(kk[i], ak[1], bf[2], bf[3]);
-                    mma_bf16(qk[k * 16 / ds][i], aq[0], bf[0], bf[1]);
-                    mma_bf16(qk[k * 16 / ds][i], aq[1], bf[2], bf[3]);
-                }
+            for (int i = 0; i < kNt; ++i) {
+                uint32_t bf[4];
+                ldmatrix_x4(k_at + (i * 8 + (lane & 7)) * L::kPitch + (2 * k + (lane >> 3)) * 16, bf);
+                mma_bf16(kk[i], ak[0], bf[0], bf[1]);
+                mma_bf16(kk[i], ak[1], bf[2], bf[3]);
+                mma_bf16(qk[k * 16 / ds][i], aq[0], bf[0], bf[1]);
+                mma_bf16(qk[k * 16 / ds][i], aq[1], bf[2], bf[3]);
             }
         }
-        __syncthreads();                          // q and k have been read: the tables take their place
-        if (warp < R) {
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int t = warp * 16 + r * 8 + g4;
-                const unsigned long long path = t < n ? nd->above[t] | 1ull << t : 0ull, seen = path & nd->keep;
-                const float bt = nd->beta[t] * nd->rk_la[t], fq = a.scale_la * nd->rq_la[t];
+        for (int r = 0; r < 2; ++r) {
+            const int t = warp * 16 + r * 8 + g4;
+            const unsigned long long path = t < n ? nd->above[t] | 1ull << t : 0ull, seen = path & nd->keep, fold = path & nd->fold;
+            const float bt = nd->beta[t] * nd->rk_la[t], fq = a.scale_la * nd->rq_la[t];
+            const float f = a.scale_sm * kLog2e * nd->rq_sm[G > 1 ? sc : 0][t];
+            float m = -INFINITY, z = 0.f, y[kNt][2];
 #pragma unroll
-                for (int i = 0; i < kNt; ++i)
+            for (int i = 0; i < kNt; ++i) {
+                float w[2];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int j = i * 8 + 2 * c4 + x;
-                        if (!(path >> j & 1)) continue;
-                        float q = qk[0][i][2 * r + x];
-#pragma unroll
-                        for (int s = 1; s < G; ++s) q += qk[s][i][2 * r + x];
-                        const float w = sb[t * kRows + j] * nd->rk_la[j];      // (the decay)
-                        sa[t * kRows + j] = bt * w * kk[i][2 * r + x];
-                        sb[t * kRows + j] = fq * w * q;
-                    }
-#pragma unroll
-                for (int s = 0; s < G; ++s) {
-                    const float f = a.scale_sm * kLog2e * nd->rq_sm[s][t];
-                    float m = -INFINITY, z = 0.f;
-#pragma unroll
-                    for (int i = 0; i < kNt; ++i)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int j = i * 8 + 2 * c4 + x;
-                            float &y = qk[s][i][2 * r + x];
-                            y = seen >> j & 1 ? y * f * nd->rk_sm[s][j] : -INFINITY;
-                            m = fmaxf(m, y);
-                        }
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-                    const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                    for (int i = 0; i < kNt; ++i) {
-                        const float p0 = tc::ex2_ftz(qk[s][i][2 * r] - mu), p1 = tc::ex2_ftz(qk[s][i][2 * r + 1] - mu);
-                        z += p0 + p1;
-                        // (fp16: 2^-11 of a probability, finer than the bf16 of those over the cache)
-                        *reinterpret_cast<uint32_t *>(sp + (s * kRows + t) * kRows + i * 8 + 2 * c4) = tc::pack_half2(p0, p1);
-                    }
-                    z += __shfl_xor_sync(0xffffffffu, z, 1);
-                    z += __shfl_xor_sync(0xffffffffu, z, 2);
-                    if (c4 == 0 && t < n) { own[s * T + t] = m; own[(4 + s) * T + t] = z; }
+                for (int x = 0; x < 2; ++x) {
+                    const int j = i * 8 + 2 * c4 + x;
+                    float q = qk[0][i][2 * r + x];
+                    y[i][x] = G > 1 && sc ? qk[G - 1][i][2 * r + x] : q;
+                    if (G > 1) q += qk[G - 1][i][2 * r + x];
+                    const float decay = fold >> j & 1 ? tab[t * kRows + j] * nd->rk_la[j] : 0.f;
+                    w[x] = fold >> j & 1 ? fq * decay * q : 0.f;
+                    if (j < t) tab[j * kRows + t] = fold >> j & 1 ? bt * decay * kk[i][2 * r + x] : 0.f;
+                    y[i][x] = seen >> j & 1 ? y[i][x] * f * nd->rk_sm[G > 1 ? sc : 0][j] : -INFINITY;
+                    m = fmaxf(m, y[i][x]);
                 }
+                uint32_t w2[2];
+                split2(w[0], w[1], w2);
+                bh_f[i / 2][(i & 1) * 2 + r] = w2[0];
+                bl_f[i / 2][(i & 1) * 2 + r] = w2[1];
+            }
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int i = 0; i < kNt; ++i) {
+                const float p0 = tc::ex2_ftz(y[i][0] - mu), p1 = tc::ex2_ftz(y[i][1] - mu);
+                z += p0 + p1;
+                p_f[i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
+            }
+            z += __shfl_xor_sync(0xffffffffu, z, 1);
+            z += __shfl_xor_sync(0xffffffffu, z, 2);
+            if (c4 == 0) { sums->tree_m[sc][t] = m; sums->tree_z[sc][t] = z; }
+        }
+    }
+
+    // ---- k S0 and q S0, a warp's tiles of eight columns for all rows ----
+    constexpr int kUnits = (L::kCols / 8 + 3) / 4;
+    float acc[kUnits][2 * R][4];
+#pragma unroll
+    for (int un = 0; un < kUnits; ++un) {
+        const int tile = warp + 4 * un;
+        if (tile >= tiles) break;
+        if (un) load(tile, s);
+#pragma unroll
+        for (int m = 0; m < 2 * R; ++m)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) acc[un][m][x] = 0.f;
+#pragma unroll
+        for (int k = 0; k < kKs; ++k) {
+            uint32_t b0[3], b1[3];
+            split3(s[k][0], s[k][1], b0);
+            split3(s[k][2], s[k][3], b1);
+#pragma unroll
+            for (int m = 0; m < 2 * R; ++m) {
+                uint32_t af[4];
+                ldmatrix_x4((m < R ? k_at : q_at) + ((m % R) * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af);
+#pragma unroll
+                for (int x = 2; x >= 0; --x) mma_bf16(acc[un][m], af, b0[x], b1[x]);
             }
         }
     }
+    __syncthreads();                              // q and k have been read: the right-hand sides and q S0 take their places
+#pragma unroll
+    for (int un = 0; un < kUnits; ++un) {
+        const int tile = warp + 4 * un, at = tile * 8 + 2 * c4;
+        if (tile >= tiles) break;
+#pragma unroll
+        for (int m = 0; m < 2 * R; ++m)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int t = (m % R) * 16 + r * 8 + g4;
+                const float x0 = acc[un][m][2 * r], x1 = acc[un][m][2 * r + 1];
+                if (m < R) {
+                    const float fk = nd->whole[t] * nd->rk_la[t], bt = nd->beta[t];
+                    const float2 v = bf2(*reinterpret_cast<const uint32_t *>(sm + L::oV + t * L::kPitchV + at * 2));
+                    *reinterpret_cast<float2 *>(su + t * cols + at) =
+                        t < n ? make_float2(bt * (v.x - fk * x0), bt * (v.y - fk * x1)) : make_float2(0.f, 0.f);
+                } else {
+                    const float fq = a.scale_la * nd->whole[t] * nd->rq_la[t];
+                    *reinterpret_cast<float2 *>(so + t * cols + at) = make_float2(fq * x0, fq * x1);
+                }
+            }
+    }
     __syncthreads();
-    // up the tree node by node; a column's thread needs no other column
-    if (tid < D) {
-        const int col = tid, gc = col / ds;
-        const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(sm + L::oV) + col;
-        const unsigned long long fold = nd->fold, keep = nd->keep;
-        constexpr int kAhead = 8;
-        float next[kAhead];
+    // ---- the substitution: a thread's column, by blocks of 16 nodes.  A node that u_j does not reach has a zero in the table;
+    // where u_j is not finite, the paths are asked. ----
+    if (tid < cols) {
+        const unsigned long long fold = nd->fold;
+        float *col = su + tid;
+        for (int t0 = 0; t0 < n; t0 += 16) {
+            float r[16];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) next[i] = i < n ? base[(size_t)i * D + col] : 0.f;
-        for (int t0 = 0; t0 < n; t0 += kAhead) {
-            float o8[kAhead];
+            for (int i = 0; i < 16; ++i) r[i] = col[(t0 + i) * cols];
+#pragma unroll 4
+            for (int j = 0; j < t0; ++j) {
+                const float u = col[j * cols], *row = tab + j * kRows + t0;
+                if (finite(u)) {
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                o8[i] = next[i];
-                next[i] = t0 + kAhead + i < n ? base[(size_t)(t0 + kAhead + i) * D + col] : 0.f;
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 w = *reinterpret_cast<const float4 *>(row + i);
+                        r[i] = fmaf(-w.x, u, r[i]); r[i + 1] = fmaf(-w.y, u, r[i + 1]);
+                        r[i + 2] = fmaf(-w.z, u, r[i + 2]); r[i + 3] = fmaf(-w.w, u, r[i + 3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (nd->above[t0 + i] >> j & 1) r[i] = fmaf(-row[i], u, r[i]);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int t = t0 + i;
-                if (t >= n) break;
-                float u = su[t * D + col], o = o8[i], s = 0.f;
-                for (unsigned long long w = nd->above[t]; w; w &= w - 1) {
-                    const int j = __ffsll(w) - 1;
-                    if (fold >> j & 1) {
-                        const float x = su[j * D + col];
-                        u = fmaf(-sa[t * kRows + j], x, u);
-                        o = fmaf(sb[t * kRows + j], x, o);
+            for (int j = 0; j < 16; ++j) {
+                const float u = r[j] = fold >> (t0 + j) & 1 ? r[j] : 0.f, *row = tab + (t0 + j) * kRows + t0;
+                if (finite(u)) {
+#pragma unroll
+                    for (int i = (j + 1) / 4 * 4; i < 16; i += 4) {
+                        const float4 w = *reinterpret_cast<const float4 *>(row + i);
+                        if (i > j) r[i] = fmaf(-w.x, u, r[i]);
+                        if (i + 1 > j) r[i + 1] = fmaf(-w.y, u, r[i + 1]);
+                        if (i + 2 > j) r[i + 2] = fmaf(-w.z, u, r[i + 2]);
+                        if (i + 3 > j) r[i + 3] = fmaf(-w.w, u, r[i + 3]);
                     }
-                    if (keep >> j & 1) s = fmaf(__half2float(sp[(gc * kRows + t) * kRows + j]), to_f32(v[j * (L::kPitch / 2)]), s);
+                } else {
+                    odd = true;
+#pragma unroll
+                    for (int i = j + 1; i < 16; ++i)
+                        if (nd->above[t0 + i] >> (t0 + j) & 1) r[i] = fmaf(-row[i], u, r[i]);
                 }
-                if (fold >> t & 1) o = fmaf(sb[t * kRows + t], u, o);
-                else u = 0.f;
-                if (keep >> t & 1) s = fmaf(__half2float(sp[(gc * kRows + t) * kRows + t]), to_f32(v[t * (L::kPitch / 2)]), s);
-                su[t * D + col] = u;
-                base[(size_t)t * D + col] = o;
-                own[8 * T + (size_t)t * D + col] = s;
-                if (a.u) a.u[(((size_t)b * T + t) * a.H + h) * D + col] = u;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) col[(t0 + i) * cols] = r[i];
+        }
+    }
+    odd = __syncthreads_or(odd);
+    if (a.u)
+        for (int i = tid; i < n * (cols / 4); i += kThreads) {
+            const int t = i / (cols / 4), c = (i - t * (cols / 4)) * 4;
+            *reinterpret_cast<float4 *>(a.u + (((size_t)b * T + t) * a.H + h) * D + c0 + c) =
+                *reinterpret_cast<const float4 *>(su + t * cols + c);
+        }
+    // ---- the read-outs.  (A row's own non-finite entries spoil that row alone; those of u and V are taken as zeros here and
+    // added below to the rows that see them.) ----
+    auto clean = [&](float x) { return odd && !finite(x) ? 0.f : x; };
+    if (warp < R) {
+        for (int tile = 0; tile < tiles; ++tile) {
+            const int at = tile * 8 + 2 * c4;
+            float o[4];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float2 y = *reinterpret_cast<const float2 *>(so + (warp * 16 + r * 8 + g4) * cols + at);
+                o[2 * r] = y.x;
+                o[2 * r + 1] = y.y;
+            }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (k > warp) break;              // (parents come first)
+                const float *y = su + (k * 16 + 2 * c4) * cols + tile * 8 + g4;
+                uint32_t b0[2], b1[2];
+                split2(clean(y[0]), clean(y[cols]), b0);
+                split2(clean(y[8 * cols]), clean(y[9 * cols]), b1);
+                mma_bf16(o, bl_f[k], b0[0], b1[0]);
+                mma_bf16(o, bh_f[k], b0[1], b1[1]);
+                mma_bf16(o, bh_f[k], b0[0], b1[0]);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                *reinterpret_cast<float2 *>(so + (warp * 16 + r * 8 + g4) * cols + at) = make_float2(o[2 * r], o[2 * r + 1]);
+        }
+    }
+    // x (hi + lo) of the A fragments, as a table [t][j] in the table's place
+    auto dump = [&](const uint32_t (&hi)[kNt / 2][4], const uint32_t (&lo)[kNt / 2][4], bool both) {
+        __syncthreads();
+        if (warp < R)
+#pragma unroll
+            for (int k = 0; k < kNt / 2; ++k)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float2 y = bf2(hi[k][x]), w = both ? bf2(lo[k][x]) : make_float2(0.f, 0.f);
+                    float *to = tab + (warp * 16 + (x & 1) * 8 + g4) * kRows + k * 16 + (x >> 1) * 8 + 2 * c4;
+                    to[0] = y.x + w.x;
+                    to[1] = y.y + w.y;
+                }
+        __syncthreads();
+    };
+    float *s_to = odd ? su : st;
+    if (odd) {
+        dump(bh_f, bl_f, true);
+        for (int i = tid; i < n * cols; i += kThreads) {
+            const int t = i / cols, c = i - t * cols;
+            for (unsigned long long w = (nd->above[t] | 1ull << t) & nd->fold; w; w &= w - 1) {
+                const int j = __ffsll(w) - 1;
+                if (!finite(su[j * cols + c])) so[i] += tab[t * kRows + j] * su[j * cols + c];
             }
         }
+        dump(p_f, p_f, false);
+    }
+    if (warp < R) {
+        for (int tile = 0; tile < tiles; ++tile) {
+            float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (k > warp) break;
+                uint32_t bf[2];
+                ldmatrix_x2_trans(v_at + (k * 16 + (lane & 15)) * L::kPitchV + tile * 16, bf);
+                if (odd)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if ((bf[x] & 0x7f80u) == 0x7f80u) bf[x] &= 0xffff0000u;
+                        if ((bf[x] & 0x7f800000u) == 0x7f800000u) bf[x] &= 0xffffu;
+                    }
+                mma_bf16(o, p_f[k], bf[0], bf[1]);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                *reinterpret_cast<float2 *>(s_to + (warp * 16 + r * 8 + g4) * cols + tile * 8 + 2 * c4) = make_float2(o[2 * r], o[2 * r + 1]);
+        }
+    }
+    if (odd) {
+        __syncthreads();
+        for (int i = tid; i < n * cols; i += kThreads) {
+            const int t = i / cols, c = i - t * cols;
+            for (unsigned long long w = (nd->above[t] | 1ull << t) & nd->keep; w; w &= w - 1) {
+                const int j = __ffsll(w) - 1;
+                const float v = to_f32(*reinterpret_cast<const __nv_bfloat16 *>(sm + L::oV + j * L::kPitchV + c * 2));
+                if (!finite(v)) su[i] += tab[t * kRows + j] * v;
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < n * cols; i += kThreads) st[i] = su[i];
     }
 }
 
 template <int D, int G, bool kNorm, int R>
 __global__ void __launch_bounds__(kThreads, 2) tree_tc_kernel(Args a) {
+    using L = Layout<D, R>;
     extern __shared__ __align__(128) uint8_t dyn_tc[];
     __shared__ Nodes nodes;
-    const int per_pair = a.parts + 1, bh = blockIdx.x / per_pair, part = blockIdx.x - bh * per_pair - 1;   // part -1: the tree
-    const int b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
-    if (part < 0) {
-        tree_item<D, G, kNorm, R>(a, dyn_tc, &nodes, b, h, n);
-    } else {
-        const Cut c = cut_of(a.cache_len[bh], a.cap, a.parts, a.least_tiles);
-        if (part < c.np && n > 0) cache_item<D, G, kNorm, R>(a, dyn_tc, b, h, part, n, c);
+    const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
+    Sums *sums = reinterpret_cast<Sums *>(dyn_tc);
+    if (n > 0) {                                  // (the same for the whole cluster)
+        cache_part<D, G, kNorm, R>(a, sums, dyn_tc, b, h, n, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
+        tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank);
+    } else if (threadIdx.x == 0 && a.n_nodes && a.n_nodes[b] != n) {
+        atomicMin(a.status, (int)NATSL_ERR_TREE);
     }
-    if (last_of_pair(a, bh)) join_pair<__nv_bfloat16, D>(a, b, h, n);
+    join_rows<__nv_bfloat16, D>(a, b, h, n, rank, sums, reinterpret_cast<const float *>(dyn_tc + L::oAcc), L::kAccPitch,
+                                reinterpret_cast<const float *>(dyn_tc + L::oK), reinterpret_cast<const float *>(dyn_tc + L::oTab));
 }
 
 template <int D, int G, bool kNorm, int R>
@@ -563,9 +679,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     auto kernel = tree_tc_kernel<D, G, kNorm, R>;
     cudaError_t e = allow_smem(kernel, Layout<D, R>::kTotal);
     if (e != cudaSuccess) return e;
-    kernel<<<BH * (a.parts + 1), kThreads, Layout<D, R>::kTotal, st>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    return launch_clusters(kernel, a, BH, Layout<D, R>::kTotal, st);
 }
 template <int D, int G, bool kNorm>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
