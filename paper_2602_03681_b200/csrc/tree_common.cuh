@@ -16,8 +16,6 @@ namespace natsl {
 namespace tree {
 
 constexpr int kMaxNodes = 64;        // one machine word of ancestors per node
-constexpr int kThreads = 128;
-constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
@@ -43,44 +41,41 @@ __device__ __forceinline__ Share share_of(int n_raw, int cap, int cluster, int r
     return Share{from, (int)min((long long)from + (long long)per * 16, (long long)n)};
 }
 
-// Head of a CTA's dynamic shared memory, read by the whole cluster: running maxima (base 2) and sums of the CTA's cache share,
-// and those of the softmax over the tree's own tokens for the softmax heads of the CTA's columns.
-struct Sums { float cache_m[4][kMaxNodes], cache_z[4][kMaxNodes], tree_m[4][kMaxNodes], tree_z[4][kMaxNodes]; };
-
-struct Nodes {
-    unsigned long long above[kMaxNodes];          // strict ancestors
-    unsigned long long fold, keep;                // nodes that update the state; nodes whose K/V count as retained
-    float beta[kMaxNodes], alpha[kMaxNodes], whole[kMaxNodes];   // whole: decay from the context up to and with the node
-    float rq_la[kMaxNodes], rk_la[kMaxNodes];     // L2 factors; RMS factors per softmax head
-    float rq_sm[4][kMaxNodes], rk_sm[4][kMaxNodes];
-    int parent[kMaxNodes];
+// Read by the whole cluster: running maxima (base 2) and sums of the CTA's cache share, and those of the softmax over the tree's
+// own tokens for the softmax heads of the CTA's columns.
+template <int kHeads, int kRows> struct Sums {
+    float cache_m[kHeads][kRows], cache_z[kHeads][kRows], tree_m[kHeads][kRows], tree_z[kHeads][kRows];
 };
 
-// Nodes of a sequence's tree; a count outside [0, T] counts as the nearer of both and is reported.
-__device__ __forceinline__ int nodes_of(const Args &a, int b) {
-    const int n = a.n_nodes ? a.n_nodes[b] : a.T;
-    return min(max(n, 0), a.T);
-}
+template <int kHeads, int kRows> struct Nodes {
+    unsigned long long above[kRows];              // strict ancestors
+    unsigned long long fold, keep;                // nodes that update the state; nodes whose K/V count as retained
+    double total[kRows];                          // sum of g from the context up to and with the node, -inf left out ...
+    int wipes[kRows];                             // ... and counted here
+    float whole[kRows], beta[kRows], g[kRows];    // whole: exp of that sum
+    float rq_la[kRows], rk_la[kRows];             // L2 factors; RMS factors per softmax head
+    float rq_sm[kHeads][kRows], rk_sm[kHeads][kRows];
+    int parent[kRows];
+};
 
-// Reads the tree of (b, h) into `nd`, walks every node's path (a parent is always a lower index, so a walk ends) and puts
-// the decay D_ij = exp(sum of g on the path from j, exclusive, to i) of every ancestor j of i at decay[i * pitch + j]:
-// products along the path, so that a decay of zero (g = -inf) stays zero and long paths lose nothing by cancellation.
-__device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, Nodes *nd, float *decay, int pitch) {
-    const int tid = threadIdx.x;
-    if (tid < kMaxNodes) {
+// Reads the tree of (b, h) and walks every node's path (a parent is always a lower index, so a walk ends).  tid: of kRows
+// threads or more, whose barrier `sync` is.
+template <int kHeads, int kRows, typename Sync>
+__device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, int tid, Nodes<kHeads, kRows> *nd, Sync sync) {
+    if (tid < 64) {                               // (two whole warps, for the ballots)
         int par = -1, rv = 0;
         if (tid < n) {
             const size_t at = ((size_t)b * a.T + tid) * a.H + h;
             par = a.parent[(size_t)b * a.T + tid];
+            rv = a.route[at];
+            nd->beta[tid] = a.beta[at];
+            nd->g[tid] = a.g[at];
             if (par < -1 || par >= tid) {         // not a tree: reported, and taken as a child of the context
                 par = -1;
                 atomicMin(a.status, (int)NATSL_ERR_TREE);
             }
-            rv = a.route[at];
-            nd->beta[tid] = a.beta[at];
-            nd->alpha[tid] = expf(a.g[at]);
         }
-        nd->parent[tid] = par;
+        if (tid < kRows) nd->parent[tid] = par;
         const unsigned f = __ballot_sync(0xffffffffu, tid < n && rv != 1), k = __ballot_sync(0xffffffffu, tid < n && rv != 0);
         if ((tid & 31) == 0) {
             reinterpret_cast<unsigned *>(&nd->fold)[tid >> 5] = f;
@@ -92,23 +87,42 @@ __device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, N
         const int len = a.cache_len[(size_t)b * a.H + h];
         if (len < 0 || len > a.cap) atomicMin(a.status, (int)NATSL_ERR_CACHE_FULL);
     }
-    __syncthreads();
-    if (tid < n) {
+    sync();
+    if (tid < kRows) {
         unsigned long long up = 0;
-        float prod = nd->alpha[tid];
-        for (int x = nd->parent[tid]; x >= 0; x = nd->parent[x]) {
-            up |= 1ull << x;
-            decay[tid * pitch + x] = prod;
-            prod *= nd->alpha[x];
+        double sum = 0.0;
+        int wipes = 0;
+        if (tid < n) {
+            auto add = [&](int x) {
+                const float g = nd->g[x];
+                if (g == -INFINITY) ++wipes;
+                else sum += g;
+            };
+            add(tid);
+            for (int x = nd->parent[tid]; x >= 0; x = nd->parent[x]) {
+                up |= 1ull << x;
+                add(x);
+            }
+        } else {
+            nd->beta[tid] = 0.f;
         }
-        decay[tid * pitch + tid] = 1.f;
         nd->above[tid] = up;
-        nd->whole[tid] = prod;
-    } else if (tid < kMaxNodes) {
-        nd->above[tid] = 0;
-        nd->whole[tid] = 0.f;
-        nd->beta[tid] = 0.f;
+        nd->total[tid] = sum;
+        nd->wipes[tid] = wipes;
+        nd->whole[tid] = wipes || tid >= n ? 0.f : expf((float)sum);
     }
+}
+// Decay on the path from its node j (exclusive) to i: the sums' difference in 64 bits, where nothing of a short stretch far from
+// the context is lost, and zero as soon as a g of -inf lies on it.
+template <int kHeads, int kRows>
+__device__ __forceinline__ float decay_of(const Nodes<kHeads, kRows> *nd, int i, int j) {
+    return nd->wipes[i] != nd->wipes[j] ? 0.f : expf((float)(nd->total[i] - nd->total[j]));
+}
+
+// Nodes of a sequence's tree; a count outside [0, T] counts as the nearer of both and is reported.
+__device__ __forceinline__ int nodes_of(const Args &a, int b) {
+    const int n = a.n_nodes ? a.n_nodes[b] : a.T;
+    return min(max(n, 0), a.T);
 }
 
 // The cluster's barrier: what its threads have written to shared memory is there for all of them.
@@ -136,44 +150,44 @@ template <int V> __device__ __forceinline__ void ld_remote(uint32_t p, float (&x
 // Joins the rows rank, rank + cluster, ... of pair (b, h): softmax over the cache shares and the tree, both branches normalised
 // and combined.  A warp takes a row; lane l owns columns V l .. V l + V - 1.  acc [rows][acc_pitch]: the CTA's sums over its
 // cache share, all columns; o_la, o_tree [rows][D / cluster]: the linear read-out and the sums over the tree, its own columns.
-template <typename ST, int D>
-__device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, int rank, const Sums *sums, const float *acc, int acc_pitch,
-                                          const float *o_la, const float *o_tree) {
-    constexpr int V = D / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.G, ls = 32 / G, sg = lane / ls, cols = D / a.cluster;
+template <typename ST, int D, int kCluster, typename S>
+__device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n, int rank, const S *sums, const float *acc,
+                                             int acc_pitch, const float *o_la, const float *o_tree) {
+    constexpr int V = D / 32, cols = D / kCluster;
+    const int lane = threadIdx.x & 31, G = a.G, ls = 32 / G, sg = lane / ls, step = kCluster * (blockDim.x >> 5);
     const int owner = lane * V / cols, at = lane * V - owner * cols;
+    int t = rank + kCluster * (threadIdx.x >> 5);
+    float2 w = make_float2(0.5f, 0.5f), w_next = w;
+    auto weights = [&](int t) { return *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t) * a.H + h) * 2); };
+    if (a.w && t < n) w_next = weights(t);
     cluster_sync();
-    for (int t = rank + a.cluster * warp; t < n; t += a.cluster * (kThreads / 32)) {
-        const size_t row = ((size_t)b * a.T + t) * a.H + h;
-        const float wn = a.w ? a.w[row * 2] : 0.5f, wl = a.w ? a.w[row * 2 + 1] : 0.5f;
-        float m[kMaxCluster], z[kMaxCluster], x[kMaxCluster][V], o[V], ol[V];
+    for (; t < n; t += step) {
+        w = w_next;
+        if (a.w && t + step < n) w_next = weights(t + step);
+        float m[kCluster], z[kCluster], x[kCluster][V], o[V], ol[V];
 #pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r) {
-            m[r] = -INFINITY;
-            if (r < a.cluster) {
-                m[r] = ld_remote(remote(&sums->cache_m[sg][t], r));
-                z[r] = ld_remote(remote(&sums->cache_z[sg][t], r));
-                ld_remote<V>(remote(acc + t * acc_pitch + lane * V, r), x[r]);
-            }
+        for (int r = 0; r < kCluster; ++r) {
+            m[r] = ld_remote(remote(&sums->cache_m[sg][t], r));
+            z[r] = ld_remote(remote(&sums->cache_z[sg][t], r));
+            ld_remote<V>(remote(acc + t * acc_pitch + lane * V, r), x[r]);
         }
         const float mt = ld_remote(remote(&sums->tree_m[sg][t], owner)), zt = ld_remote(remote(&sums->tree_z[sg][t], owner));
         ld_remote<V>(remote(o_tree + t * cols + at, owner), o);
         ld_remote<V>(remote(o_la + t * cols + at, owner), ol);
         float M = mt;
 #pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r) M = fmaxf(M, m[r]);
+        for (int r = 0; r < kCluster; ++r) M = fmaxf(M, m[r]);
         const float Mu = M == -INFINITY ? 0.f : M, ft = tc::ex2_ftz(mt - Mu);
         float Z = zt * ft;
 #pragma unroll
         for (int i = 0; i < V; ++i) o[i] *= ft;
 #pragma unroll
-        for (int r = 0; r < kMaxCluster; ++r)
-            if (r < a.cluster) {
-                const float f = tc::ex2_ftz(m[r] - Mu);
-                Z = fmaf(z[r], f, Z);
+        for (int r = 0; r < kCluster; ++r) {
+            const float f = tc::ex2_ftz(m[r] - Mu);
+            Z = fmaf(z[r], f, Z);
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = fmaf(x[r][i], f, o[i]);
-            }
+            for (int i = 0; i < V; ++i) o[i] = fmaf(x[r][i], f, o[i]);
+        }
         const float iz = Z == 0.f ? 0.f : 1.f / Z;     // (no visible key: o_nla = 0)
         float sn = 0.f, sl = 0.f;
 #pragma unroll
@@ -184,8 +198,8 @@ __device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, in
         }
         for (int s = ls / 2; s > 0; s >>= 1) sn += __shfl_xor_sync(0xffffffffu, sn, s);
         sl = warp_sum(sl);
-        const float fn = wn * rsqrtf(sn / (D / G) + a.eps), fl = wl * rsqrtf(sl / D + a.eps);
-        ST *out = reinterpret_cast<ST *>(a.out) + row * D + lane * V;
+        const float fn = w.x * rsqrtf(sn / (D / G) + a.eps), fl = w.y * rsqrtf(sl / D + a.eps);
+        ST *out = reinterpret_cast<ST *>(a.out) + (((size_t)b * a.T + t) * a.H + h) * D + lane * V;
         float y[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) y[i] = fmaf(fn, o[i], fl * ol[i]);
@@ -200,12 +214,19 @@ __device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, in
     }
     cluster_sync();                               // nobody's shared memory goes while a neighbour still reads it
 }
+template <typename ST, int D, typename S>
+__device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, int rank, const S *sums, const float *acc, int acc_pitch,
+                                          const float *o_la, const float *o_tree) {
+    if (a.cluster == 2) join_rows_of<ST, D, 2>(a, b, h, n, rank, sums, acc, acc_pitch, o_la, o_tree);
+    else if (a.cluster == 4) join_rows_of<ST, D, 4>(a, b, h, n, rank, sums, acc, acc_pitch, o_la, o_tree);
+    else join_rows_of<ST, D, 8>(a, b, h, n, rank, sums, acc, acc_pitch, o_la, o_tree);
+}
 
 // One cluster per pair.
-template <typename K> cudaError_t launch_clusters(K kernel, const Args &a, int BH, size_t smem, cudaStream_t st) {
+template <typename K> cudaError_t launch_clusters(K kernel, const Args &a, int BH, int threads, size_t smem, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(BH * a.cluster);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];

@@ -18,9 +18,11 @@ namespace {
 using namespace tree;
 
 constexpr int kKeys = 32;                         // keys per tile: one per lane
-constexpr int kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+using SimtSums = Sums<4, kMaxNodes>;
+using SimtNodes = Nodes<4, kMaxNodes>;
 
-constexpr int kHead = sizeof(Sums) / 4;           // floats; then acc [T][D + 4], then what one of the two parts needs:
+constexpr int kHead = sizeof(SimtSums) / 4;           // floats; then acc [T][D + 4], then what one of the two parts needs:
 __host__ __device__ inline int acc_floats(int T, int D) { return T * (D + 4); }
 // the tree's part: o_la, o_tree, u (own columns); q, k; two tables and the probabilities of the columns' softmax heads
 __host__ __device__ inline int tree_floats(int T, int D, int G, int cluster) {
@@ -34,7 +36,7 @@ __host__ __device__ inline int cache_floats(int TT, int D, int G) {
 // The CTA's share of the cache.  Lane = key for the logits (a warp owns whole rows of a tile, so maximum and sum are shuffles), thread =
 // column for the products with V (RC rows of accumulators).
 template <typename ST, int D, int TT>
-__device__ void cache_part(const Args &a, Sums *sums, float *out_acc, float *sm, int b, int h, int n_nodes, const Share &c) {
+__device__ void cache_part(const Args &a, SimtSums *sums, float *out_acc, float *sm, int b, int h, int n_nodes, const Share &c) {
     constexpr int RC = TT * D / 128, P = D + 4;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G;
     const int bh = b * a.H + h;
@@ -138,7 +140,7 @@ __device__ void cache_part(const Args &a, Sums *sums, float *out_acc, float *sm,
 
 // The tree's own part, for the columns c0 .. c0 + D / cluster - 1.
 template <typename ST, int D>
-__device__ void tree_part(const Args &a, Sums *sums, float *sm, Nodes *nd, int b, int h, int n, int rank) {
+__device__ void tree_part(const Args &a, SimtSums *sums, float *sm, SimtNodes *nd, int b, int h, int n, int rank) {
     constexpr int P = D + 4;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.G, ds = D / G, T = a.T, cols = D / a.cluster, c0 = rank * cols;
     const int g0 = c0 / ds, heads = (c0 + cols - 1) / ds - g0 + 1;       // softmax heads that these columns belong to
@@ -151,7 +153,7 @@ __device__ void tree_part(const Args &a, Sums *sums, float *sm, Nodes *nd, int b
         sq[t * P + x] = to_f32(reinterpret_cast<const ST *>(a.q)[at]);
         sk[t * P + x] = to_f32(reinterpret_cast<const ST *>(a.k)[at]);
     }
-    read_nodes(a, b, h, n, nd, sb, T);
+    read_nodes(a, b, h, n, tid, nd, [] { __syncthreads(); });
     __syncthreads();
     for (int t = warp; t < n; t += kWarps) {      // the rows' norms: lanes of a softmax head's columns together
         float xq = 0.f, xk = 0.f;
@@ -207,7 +209,7 @@ __device__ void tree_part(const Args &a, Sums *sums, float *sm, Nodes *nd, int b
             so[t * cols + col] = a.scale_la * nd->whole[t] * nd->rq_la[t] * aq[r];
         }
     }
-    // the tables, where j is above i or i itself (sb holds the decays)
+    // the tables, where j is above i or i itself
     for (int i = tid; i < n * n; i += kThreads) {
         const int t = i / n, j = i - t * n;
         if (j > t || !((nd->above[t] | 1ull << t) >> j & 1)) continue;
@@ -223,7 +225,7 @@ __device__ void tree_part(const Args &a, Sums *sums, float *sm, Nodes *nd, int b
             if (g >= g0 && g < g0 + heads) sp[((g - g0) * T + t) * T + j] = a.scale_sm * kLog2e * nd->rq_sm[g][t] * nd->rk_sm[g][j] * qg;
             qk += qg;
         }
-        const float dec = sb[t * T + j];
+        const float dec = decay_of(nd, t, j);
         sa[t * T + j] = nd->beta[t] * dec * nd->rk_la[t] * nd->rk_la[j] * kk;
         sb[t * T + j] = a.scale_la * dec * nd->rq_la[t] * nd->rk_la[j] * qk;
     }
@@ -271,9 +273,9 @@ __device__ void tree_part(const Args &a, Sums *sums, float *sm, Nodes *nd, int b
 template <typename ST, int D, int TT>
 __global__ void __launch_bounds__(kThreads) tree_simt_kernel(Args a) {
     extern __shared__ __align__(16) float dyn[];
-    __shared__ Nodes nodes;
+    __shared__ SimtNodes nodes;
     const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
-    Sums *sums = reinterpret_cast<Sums *>(dyn);
+    SimtSums *sums = reinterpret_cast<SimtSums *>(dyn);
     float *acc = dyn + kHead, *work = acc + acc_floats(a.T, D);
     cache_part<ST, D, TT>(a, sums, acc, work, b, h, n, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
     __syncthreads();
@@ -288,7 +290,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     };
     cudaError_t e = allow_smem(tree_simt_kernel<ST, D, TT>, bytes(TT, D / 32, 2));
     if (e != cudaSuccess) return e;
-    return launch_clusters(tree_simt_kernel<ST, D, TT>, a, BH, bytes(a.T, a.G, a.cluster), st);
+    return launch_clusters(tree_simt_kernel<ST, D, TT>, a, BH, kThreads, bytes(a.T, a.G, a.cluster), st);
 }
 template <typename ST, int D>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
@@ -303,8 +305,8 @@ size_t tree_workspace_bytes() { return 256; }
 
 cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool tensor_cores, cudaStream_t st) {
     const int BH = s.B * s.H;
-    // CTAs per pair: as many as one resident set of two per multiprocessor has for each
-    const int cluster = BH * 8 <= 2 * 148 ? 8 : BH * 4 <= 2 * 148 ? 4 : 2;
+    // CTAs per pair: as many as one resident set (one CTA per multiprocessor beyond 32 nodes, else two) has for each
+    const int resident = s.L > 32 ? 148 : 2 * 148, cluster = BH * 8 <= resident ? 8 : BH * 4 <= resident ? 4 : 2;
     const Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
                  c.out, c.u, c.lse, (int32_t *)c.ws, s.H, s.L, c.cap, hg.G, cluster, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
     if (tensor_cores && hg.G <= 2) return launch_tree_tc(a, BH, s.d, st);

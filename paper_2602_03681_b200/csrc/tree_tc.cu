@@ -2,13 +2,13 @@
 // tree_simt.cu's; here the products are warp-level MMAs: a tree has 1 to 64 query rows, far below a tcgen05 tile of 128, and
 // the call is bound by reading the retained K/V once.
 //
-// The cache's share of a CTA streams in tiles of 64 keys through a ring of asynchronous copies.  The four warps share the tile
-// by keys (and, beyond 32 nodes, by two halves of the rows), each with its own running maximum and sum, so that a key's row
-// leaves shared memory once (twice) whatever the number of nodes; the warps' results meet at the end.  A running maximum
-// moves only when a logit exceeds it by 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's own precision);
-// their sum is taken before the rounding.
+// A CTA has two halves that work side by side and meet at the end.  Four warps read the CTA's share of the cache: tiles of 64
+// keys through a ring of asynchronous copies, K and V in turns.  They share the tile by keys (and, beyond 16 nodes, by two
+// halves of the rows), each with its own running maximum and sum, so that a key's row leaves shared memory once (twice)
+// whatever the number of nodes; the warps' results meet at the end.  A running maximum moves only when a logit exceeds it by
+// 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's own precision); their sum is taken before the rounding.
 //
-// The tree's own part, for a CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32 state as three bf16 terms that
+// The other four warps compute the tree's own part, for the CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32 state as three bf16 terms that
 // together hold all of its 24 bits, so that u, which goes into the state at the commit, is as exact as on CUDA cores; the
 // substitution for u in fp32, a thread per column, by blocks of 16 nodes without a look at the tree's shape (the table is
 // zero off the path); the read-outs as MMAs again, u and the table as two bf16 terms each (2^-16).  Zeros in the place of
@@ -22,7 +22,7 @@ namespace {
 
 using namespace tree;
 
-constexpr int kTileKeys = 64;
+constexpr int kThreads = 256, kHalf = 128, kTileKeys = 64;
 using tc::ldmatrix_x4;
 using tc::ldmatrix_x4_trans;
 
@@ -47,90 +47,97 @@ __device__ __forceinline__ float2 bf2(uint32_t x) { return make_float2(__uint_as
 // R: 16-row tiles that hold the tree's nodes (1, 2, 4).
 template <int D, int R> struct Layout {
     static constexpr int kRows = 16 * R;                     // nodes, padded
-    static constexpr int kMt = R < 2 ? R : 2;                // row tiles per warp
+    using S = Sums<2, kRows>;
+    using N = Nodes<2, kRows>;
+    static constexpr int kCtas = R == 4 ? 1 : 2;             // per multiprocessor
+    static constexpr int kMt = R == 4 ? 2 : 1;               // cache: row tiles per warp
     static constexpr int kRowGroups = R / kMt, kKeyGroups = 4 / kRowGroups, kWarpKeys = kTileKeys / kKeyGroups;
     static constexpr int kRowBytes = D * 2, kTileBytes = kTileKeys * kRowBytes;
-    static constexpr int kStages = D == 128 ? 3 : 4;
+    static constexpr int kSlots = R == 4 ? (D == 128 ? 7 : 8) : D == 128 ? 4 : 6;
     static constexpr int kAccPitch = D + 4;
-    static constexpr int oAcc = sizeof(Sums);                // the CTA's sums over its share of the cache
-    static constexpr int oWork = oAcc + kRows * kAccPitch * 4;
-    // while the cache is read: the ring (16-byte pieces swizzled by row), then the key groups' results over it and over oAcc
-    static constexpr int oRing = sizeof(Sums), kRing = kStages * 2 * kTileBytes, kMerge = kKeyGroups * kRows * kAccPitch * 4;
-    // the tree's part: q, k (then, in their places, u and o_la of the CTA's columns), v, the table
     static constexpr int kCols = D / 2;                      // columns of a CTA, at most
     static constexpr int kPitch = kRowBytes + 16;            // (an odd number of 16-byte pieces: eight rows, eight banks)
     static constexpr int kPitchV = kCols * 2 + 16;
-    static constexpr int oQ = oWork, oK = oQ + kRows * kPitch, oV = oK + kRows * kPitch, oTab = oV + kRows * kPitchV;
-    static constexpr int kTabBytes = kRows * (kRows > kCols ? kRows : kCols) * 4;    // (the sums over the tree's V take its place)
-    static constexpr int kTree = oTab + kTabBytes;
-    static constexpr int kStream = oRing + (kRing > kMerge ? kRing : kMerge);
-    static constexpr int kTotal = kTree > kStream ? kTree : kStream;
+    static constexpr int oQ = sizeof(S), oK = oQ + kRows * kPitch, oV = oK + kRows * kPitch, oTab = oV + kRows * kPitchV;
+    static constexpr int oO = oTab + kRows * kRows * 4, oT = oO + kRows * kCols * 4;      // the read-outs: linear, over the tree
+    // the ring (16-byte pieces swizzled by row); at the end the key groups' results, the first one's place the CTA's
+    static constexpr int oRing = (oT + kRows * kCols * 4 + 127) / 128 * 128, kRing = kSlots * kTileBytes;
+    static constexpr int kMerge = kKeyGroups * kRows * kAccPitch * 4;
+    static_assert(kMerge <= kRing, "the key groups' results lie in the ring");
+    static constexpr int kTotal = oRing + kRing;
+};
+
+// The CTA's share of the cache: units 0, 1, 2, ... are K of tile 0, V of tile 0, K of tile 1, ...
+template <int D, int R> struct Stream {
+    using L = Layout<D, R>;
+    static constexpr int kPieces = L::kRowBytes / 16, kStep = kHalf / kPieces;
+    const uint8_t *kc, *vc;
+    uint32_t ring, dst0;
+    int row0, from, to, units;
+    __device__ Stream(const Args &a, uint8_t *sm, int bh, int tid, const Share &c) {
+        const int piece = tid % kPieces;          // thread = 16-byte piece of every eighth (sixteenth) row of a tile
+        row0 = tid / kPieces;
+        kc = reinterpret_cast<const uint8_t *>(a.k_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
+        vc = reinterpret_cast<const uint8_t *>(a.v_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
+        ring = tc::smem_u32(sm + L::oRing);
+        dst0 = row0 * L::kRowBytes + ((piece ^ (row0 & 7)) << 4);
+        from = c.from;
+        to = c.to;
+        units = (c.to - c.from + kTileKeys - 1) / kTileKeys * 2;
+    }
+    __device__ uint32_t slot(int u) const { return ring + u % L::kSlots * L::kTileBytes; }
+    __device__ void fetch(int u) const {
+        if (u < units) {
+            const uint32_t at = slot(u) + dst0;
+            const uint8_t *src = u & 1 ? vc : kc;
+#pragma unroll
+            for (int i = 0; i < kTileKeys / kStep; ++i) {
+                const int j = from + (u >> 1) * kTileKeys + row0 + i * kStep;
+                const bool in = j < to;           // rows past the end count as zeros: what lies there may be anything
+                cp_async16(at + i * kStep * L::kRowBytes, src + (size_t)(in ? j : from) * L::kRowBytes, in);
+            }
+        }
+        cp_async_commit();
+    }
 };
 
 template <int D, int G, bool kNorm, int R>
-__device__ void cache_part(const Args &a, Sums *sums, uint8_t *sm, int b, int h, int n_nodes, const Share &c) {
+__device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t *sm, const Stream<D, R> &in, int n_nodes) {
     using L = Layout<D, R>;
     constexpr int ds = D / G, kMt = L::kMt, kNt = L::kWarpKeys / 8, kKs = ds / 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
     const int rg = warp / L::kKeyGroups, kg = warp - rg * L::kKeyGroups, r0 = rg * 16 * kMt;
-    const int bh = b * a.H + h;
-    const uint32_t ring = tc::smem_u32(sm + L::oRing);
+    const uint32_t q_at = tc::smem_u32(sm + L::oQ) + (r0 + (lane & 15)) * L::kPitch + (lane >> 4) * 16;
+    auto load_q = [&](int m, int k, uint32_t (&x)[4]) { ldmatrix_x4(q_at + m * 16 * L::kPitch + k * 32, x); };
 
-    // copies: thread = 16-byte piece of every eighth (sixteenth) row of a tile
-    constexpr int kPieces = L::kRowBytes / 16, kStep = kThreads / kPieces;
-    const int piece = tid % kPieces, row0 = tid / kPieces;
-    const uint8_t *kc = reinterpret_cast<const uint8_t *>(a.k_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
-    const uint8_t *vc = reinterpret_cast<const uint8_t *>(a.v_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
-    const uint32_t dst0 = row0 * L::kRowBytes + ((piece ^ (row0 & 7)) << 4);
-    const int tiles = (c.to - c.from + kTileKeys - 1) / kTileKeys;
-    auto fetch = [&](int t) {
-        if (t < tiles) {
-            const uint32_t at = ring + t % L::kStages * 2 * L::kTileBytes + dst0;
-#pragma unroll
-            for (int i = 0; i < kTileKeys / kStep; ++i) {
-                const int j = c.from + t * kTileKeys + row0 + i * kStep;
-                const bool in = j < c.to;         // rows past the end count as zeros: what lies there may be anything
-                const size_t off = (size_t)(in ? j : c.from) * L::kRowBytes;
-                cp_async16(at + i * kStep * L::kRowBytes, kc + off, in);
-                cp_async16(at + L::kTileBytes + i * kStep * L::kRowBytes, vc + off, in);
-            }
-        }
-        cp_async_commit();
-    };
-    for (int i = 0; i < L::kStages - 1; ++i) fetch(i);
-
-    // q as A fragments, and each row's factor to base-2 logits
-    uint32_t qf[kMt][D / 16][4];
+    // each row's factor to base-2 logits
     float f[kMt][2][kNorm ? G : 1];
 #pragma unroll
-    for (int m = 0; m < kMt; ++m)
+    for (int m = 0; m < kMt; ++m) {
+        f[m][0][0] = f[m][1][0] = a.scale_sm * kLog2e;
+        if (kNorm) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int t = r0 + m * 16 + r * 8 + g4;
-            const uint32_t *row = reinterpret_cast<const uint32_t *>(a.q) + (((size_t)b * a.T + min(t, n_nodes - 1)) * a.H + h) * (D / 2);
+            for (int s = 0; s < G; ++s) {
+                float ss[2] = {0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
+                for (int k = s * kKs; k < (s + 1) * kKs; ++k) {
+                    uint32_t x[4];
+                    load_q(m, k, x);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) qf[m][k][r + 2 * x] = t < n_nodes ? __ldg(row + k * 8 + x * 4 + c4) : 0u;
-            if (kNorm) {
-#pragma unroll
-                for (int s = 0; s < G; ++s) {
-                    float ss = 0.f;
-#pragma unroll
-                    for (int k = s * kKs; k < (s + 1) * kKs; ++k)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const float2 y = bf2(qf[m][k][r + 2 * x]);
-                            ss = fmaf(y.x, y.x, fmaf(y.y, y.y, ss));
-                        }
-                    ss += __shfl_xor_sync(0xffffffffu, ss, 1);
-                    ss += __shfl_xor_sync(0xffffffffu, ss, 2);
-                    f[m][r][s] = a.scale_sm * kLog2e * rsqrtf(ss / ds + a.norm_eps);
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 y = bf2(x[i]);
+                        ss[i & 1] = fmaf(y.x, y.x, fmaf(y.y, y.y, ss[i & 1]));
+                    }
                 }
-            } else {
-                f[m][r][0] = a.scale_sm * kLog2e;
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    ss[r] += __shfl_xor_sync(0xffffffffu, ss[r], 1);
+                    ss[r] += __shfl_xor_sync(0xffffffffu, ss[r], 2);
+                    f[m][r][s] = a.scale_sm * kLog2e * rsqrtf(ss[r] / ds + a.norm_eps);
+                }
             }
         }
+    }
     float o[kMt][D / 8][4], mx[G][kMt][2], z[G][kMt][2];
 #pragma unroll
     for (int m = 0; m < kMt; ++m) {
@@ -144,119 +151,130 @@ __device__ void cache_part(const Args &a, Sums *sums, uint8_t *sm, int b, int h,
             for (int r = 0; r < 2; ++r) { mx[s][m][r] = -INFINITY; z[s][m][r] = 0.f; }
     }
     const int key0 = kg * L::kWarpKeys;
-    for (int t = 0; t < tiles; ++t) {
-        cp_async_wait<L::kStages - 2>();
-        __syncthreads();                          // tile t is there, and every warp is done with tile t - 1 ...
-        fetch(t + L::kStages - 1);                // ... whose place this one takes
-        const int left = c.to - c.from - t * kTileKeys - key0;      // of the warp's keys
-        if (left <= 0) continue;
-        const uint32_t kt = ring + t % L::kStages * 2 * L::kTileBytes, vt = kt + L::kTileBytes;
+    uint32_t pf[G][kMt][kNt / 2][4];
+    auto turn = [&](int u) {                      // unit u is there, and every warp is done with unit u - 1 ...
+        cp_async_wait<L::kSlots - 2>();
+        tc::named_barrier_sync(1, kHalf);
+        in.fetch(u + L::kSlots - 1);              // ... whose place this one takes
+    };
+    for (int u = 0; u < in.units; u += 2) {
+        const int left = in.to - in.from - (u >> 1) * kTileKeys - key0;      // of the warp's keys
+        turn(u);
+        if (left > 0) {
+            const uint32_t kt = in.slot(u);
 #pragma unroll
-        for (int s = 0; s < G; ++s) {
-            float x[kMt][kNt][4], kk[kNt];
+            for (int s = 0; s < G; ++s) {
+                float x[kMt][kNt][4], kk[kNt];
 #pragma unroll
-            for (int i = 0; i < kNt; ++i) {
-                kk[i] = 0.f;
+                for (int i = 0; i < kNt; ++i) {
+                    kk[i] = 0.f;
 #pragma unroll
-                for (int m = 0; m < kMt; ++m)
+                    for (int m = 0; m < kMt; ++m)
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) x[m][i][y] = 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < kNt; i += 2) {
-                const int row = key0 + i * 8 + (lane & 7) + (lane >> 4) * 8;
+                        for (int y = 0; y < 4; ++y) x[m][i][y] = 0.f;
+                }
 #pragma unroll
                 for (int k = s * kKs; k < (s + 1) * kKs; ++k) {
-                    uint32_t bf[4];
-                    ldmatrix_x4(kt + row * L::kRowBytes + (((2 * k + ((lane >> 3) & 1)) ^ (row & 7)) << 4), bf);
+                    uint32_t qf[kMt][4];
 #pragma unroll
-                    for (int m = 0; m < kMt; ++m) {
-                        mma_bf16(x[m][i], qf[m][k], bf[0], bf[1]);
-                        mma_bf16(x[m][i + 1], qf[m][k], bf[2], bf[3]);
-                    }
-                    if (kNorm) {                  // the key's sum of squares rides along
+                    for (int m = 0; m < kMt; ++m) load_q(m, k, qf[m]);
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const float2 w = bf2(bf[y]);
-                            kk[i + y / 2] = fmaf(w.x, w.x, fmaf(w.y, w.y, kk[i + y / 2]));
+                    for (int i = 0; i < kNt; i += 2) {
+                        const int row = key0 + i * 8 + (lane & 7) + (lane >> 4) * 8;
+                        uint32_t bf[4];
+                        ldmatrix_x4(kt + row * L::kRowBytes + (((2 * k + ((lane >> 3) & 1)) ^ (row & 7)) << 4), bf);
+#pragma unroll
+                        for (int m = 0; m < kMt; ++m) {
+                            mma_bf16(x[m][i], qf[m], bf[0], bf[1]);
+                            mma_bf16(x[m][i + 1], qf[m], bf[2], bf[3]);
+                        }
+                        if (kNorm) {              // the key's sum of squares rides along
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const float2 w = bf2(bf[y]);
+                                kk[i + y / 2] = fmaf(w.x, w.x, fmaf(w.y, w.y, kk[i + y / 2]));
+                            }
                         }
                     }
                 }
-            }
-            // logits; a lane's columns of tile i are keys 2 c4, 2 c4 + 1, its sum of squares belongs to key g4
+                // logits; a lane's columns of tile i are keys 2 c4, 2 c4 + 1, its sum of squares belongs to key g4
 #pragma unroll
-            for (int i = 0; i < kNt; ++i) {
-                float w0 = 1.f, w1 = 1.f;
-                if (kNorm) {
-                    kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 1);
-                    kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 2);
-                    const float w = rsqrtf(fmaf(kk[i], 1.f / ds, a.norm_eps));
-                    w0 = __shfl_sync(0xffffffffu, w, c4 * 8);
-                    w1 = __shfl_sync(0xffffffffu, w, c4 * 8 + 4);
+                for (int i = 0; i < kNt; ++i) {
+                    float w0 = 1.f, w1 = 1.f;
+                    if (kNorm) {
+                        kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 1);
+                        kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 2);
+                        const float w = rsqrtf(fmaf(kk[i], 1.f / ds, a.norm_eps));
+                        w0 = __shfl_sync(0xffffffffu, w, c4 * 8);
+                        w1 = __shfl_sync(0xffffffffu, w, c4 * 8 + 4);
+                    }
+                    const bool in0 = i * 8 + 2 * c4 < left, in1 = i * 8 + 2 * c4 + 1 < left;
+#pragma unroll
+                    for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float fr = f[m][r][kNorm ? s : 0];
+                            x[m][i][2 * r] = in0 ? x[m][i][2 * r] * (fr * w0) : -INFINITY;
+                            x[m][i][2 * r + 1] = in1 ? x[m][i][2 * r + 1] * (fr * w1) : -INFINITY;
+                        }
                 }
-                const bool in0 = i * 8 + 2 * c4 < left, in1 = i * 8 + 2 * c4 + 1 < left;
+                bool raise = false;
+                float top[kMt][2];
 #pragma unroll
                 for (int m = 0; m < kMt; ++m)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float fr = f[m][r][kNorm ? s : 0];
-                        x[m][i][2 * r] = in0 ? x[m][i][2 * r] * (fr * w0) : -INFINITY;
-                        x[m][i][2 * r + 1] = in1 ? x[m][i][2 * r + 1] * (fr * w1) : -INFINITY;
+                        float y = x[m][0][2 * r];
+#pragma unroll
+                        for (int i = 0; i < kNt; ++i) y = tc::max3(y, x[m][i][2 * r], x[m][i][2 * r + 1]);
+                        y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
+                        top[m][r] = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
+                        raise |= top[m][r] > mx[s][m][r] + 8.f;
                     }
-            }
-            bool raise = false;
-            float top[kMt][2];
+                if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-            for (int m = 0; m < kMt; ++m)
+                    for (int m = 0; m < kMt; ++m)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    float y = x[m][0][2 * r];
+                        for (int r = 0; r < 2; ++r) {
+                            const float m1 = fmaxf(mx[s][m][r], top[m][r]);
+                            const float e = mx[s][m][r] == m1 ? 1.f : tc::ex2_ftz(mx[s][m][r] - m1);
+                            mx[s][m][r] = m1;
+                            z[s][m][r] *= e;
 #pragma unroll
-                    for (int i = 0; i < kNt; ++i) y = tc::max3(y, x[m][i][2 * r], x[m][i][2 * r + 1]);
-                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
-                    top[m][r] = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
-                    raise |= top[m][r] > mx[s][m][r] + 8.f;
+                            for (int i = s * ds / 8; i < (s + 1) * ds / 8; ++i) {
+                                o[m][i][2 * r] *= e;
+                                o[m][i][2 * r + 1] *= e;
+                            }
+                        }
                 }
-            if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
                 for (int m = 0; m < kMt; ++m)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float m1 = fmaxf(mx[s][m][r], top[m][r]);
-                        const float e = mx[s][m][r] == m1 ? 1.f : tc::ex2_ftz(mx[s][m][r] - m1);
-                        mx[s][m][r] = m1;
-                        z[s][m][r] *= e;
+                        const float mu = mx[s][m][r] == -INFINITY ? 0.f : mx[s][m][r];
 #pragma unroll
-                        for (int i = s * ds / 8; i < (s + 1) * ds / 8; ++i) {
-                            o[m][i][2 * r] *= e;
-                            o[m][i][2 * r + 1] *= e;
+                        for (int i = 0; i < kNt; ++i) {
+                            const float p0 = tc::ex2_ftz(x[m][i][2 * r] - mu), p1 = tc::ex2_ftz(x[m][i][2 * r + 1] - mu);
+                            z[s][m][r] += p0 + p1;
+                            pf[s][m][i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
                         }
                     }
             }
-            uint32_t pf[kMt][kNt / 2][4];
-#pragma unroll
-            for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const float mu = mx[s][m][r] == -INFINITY ? 0.f : mx[s][m][r];
-#pragma unroll
-                    for (int i = 0; i < kNt; ++i) {
-                        const float p0 = tc::ex2_ftz(x[m][i][2 * r] - mu), p1 = tc::ex2_ftz(x[m][i][2 * r + 1] - mu);
-                        z[s][m][r] += p0 + p1;
-                        pf[m][i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
-                    }
-                }
+        }
+        turn(u + 1);
+        if (left > 0) {
+            const uint32_t vt = in.slot(u + 1);
 #pragma unroll
             for (int i = 0; i < kNt / 2; ++i) {
                 const int row = key0 + i * 16 + (lane & 15);
 #pragma unroll
-                for (int n = s * ds / 16; n < (s + 1) * ds / 16; ++n) {
+                for (int n = 0; n < D / 16; ++n) {
                     uint32_t bf[4];
                     ldmatrix_x4_trans(vt + row * L::kRowBytes + (((2 * n + (lane >> 4)) ^ (row & 7)) << 4), bf);
 #pragma unroll
                     for (int m = 0; m < kMt; ++m) {
-                        mma_bf16(o[m][2 * n], pf[m][i], bf[0], bf[1]);
-                        mma_bf16(o[m][2 * n + 1], pf[m][i], bf[2], bf[3]);
+                        mma_bf16(o[m][2 * n], pf[n * 16 / ds][m][i], bf[0], bf[1]);
+                        mma_bf16(o[m][2 * n + 1], pf[n * 16 / ds][m][i], bf[2], bf[3]);
                     }
                 }
             }
@@ -265,8 +283,8 @@ __device__ void cache_part(const Args &a, Sums *sums, uint8_t *sm, int b, int h,
     // the key groups' results -> the CTA's
     __shared__ float s_m[G][L::kKeyGroups][L::kRows], s_z[G][L::kKeyGroups][L::kRows];
     cp_async_wait<0>();
-    __syncthreads();
-    float *acc = reinterpret_cast<float *>(sm + L::oAcc);    // the first key group's place is the result's
+    tc::named_barrier_sync(1, kHalf);
+    float *acc = reinterpret_cast<float *>(sm + L::oRing);
 #pragma unroll
     for (int m = 0; m < kMt; ++m)
 #pragma unroll
@@ -283,8 +301,8 @@ __device__ void cache_part(const Args &a, Sums *sums, uint8_t *sm, int b, int h,
                 if (c4 == 0) { s_m[s][kg][t] = mx[s][m][r]; s_z[s][kg][t] = y; }
             }
         }
-    __syncthreads();
-    for (int i = tid; i < n_nodes * (D / 4); i += kThreads) {
+    tc::named_barrier_sync(1, kHalf);
+    for (int i = tid; i < n_nodes * (D / 4); i += kHalf) {
         const int t = i / (D / 4), x = (i - t * (D / 4)) * 4, s = x / ds;
         float M = -INFINITY;
 #pragma unroll
@@ -303,7 +321,6 @@ __device__ void cache_part(const Args &a, Sums *sums, uint8_t *sm, int b, int h,
         *reinterpret_cast<float4 *>(acc + t * L::kAccPitch + x) = y;
         if (x % ds == 0) { sums->cache_m[s][t] = M; sums->cache_z[s][t] = Z; }
     }
-    __syncthreads();                              // (the other key groups' places are free)
 }
 
 // x as three bf16 terms, pairwise packed: what two rounded terms leave over is exact in the third.
@@ -326,17 +343,23 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t (&t)[2]) {
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 __device__ __forceinline__ bool finite_bf16x2(uint32_t x) { return (x & 0x7f80u) != 0x7f80u && (x & 0x7f800000u) != 0x7f800000u; }
 
-// The tree's own part, for columns c0 .. c0 + cols - 1 (cols = D / cluster).
+// The tree's own part, for columns c0 .. c0 + cols - 1 (cols = D / cluster).  q, k and the columns of v are in shared memory;
+// odd: a value of those is not finite.
 template <int D, int G, bool kNorm, int R>
-__device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int b, int h, int n, int rank) {
+__device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t *sm, typename Layout<D, R>::N *nd, int b, int h, int n,
+                          int rank, bool odd) {
     using L = Layout<D, R>;
-    constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
+    constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16, kPieces = L::kRowBytes / 16;
+    const int tid = threadIdx.x - kHalf, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
     const int bh = b * a.H + h, cols = D / a.cluster, c0 = rank * cols, sc = c0 / ds;   // sc: the columns' softmax head
-    float *tab = reinterpret_cast<float *>(sm + L::oTab);    // below the diagonal decays [i][j], above it [j][i]: what u_j takes from u_i
-    float *su = reinterpret_cast<float *>(sm + L::oQ), *so = reinterpret_cast<float *>(sm + L::oK), *st = tab;
+    auto sync = [] { tc::named_barrier_sync(2, kHalf); };
+    float *tab = reinterpret_cast<float *>(sm + L::oTab);    // [j][i], i > j: what u_i takes from u_j
+    float *su = reinterpret_cast<float *>(sm + L::oK);       // (over k)
+    float *so = reinterpret_cast<float *>(sm + L::oO), *st = reinterpret_cast<float *>(sm + L::oT);
 
     // A tile of eight state columns as the B fragments of all products with it: rows 2 c4, + 1, + 8, + 9 of a step of 16.
+    __shared__ int s_odd;
+    if (tid == 0) s_odd = 0;
     const float *S = a.state + (size_t)bh * D * D + c0 + g4;
     auto load = [&](int tile, float (&y)[kKs][4]) {
 #pragma unroll
@@ -347,24 +370,7 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
     const int tiles = cols / 8;
     float s[kKs][4];
     if (warp < tiles) load(warp, s);
-
-    constexpr int kPieces = L::kRowBytes / 16;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int i = tid; i < kRows * kPieces; i += kThreads) {
-        const int t = i / kPieces, c = i - t * kPieces;
-        const size_t at = (((size_t)b * T + min(t, n - 1)) * a.H + h) * kPieces + c;
-        *reinterpret_cast<uint4 *>(sm + L::oQ + t * L::kPitch + c * 16) = t < n ? reinterpret_cast<const uint4 *>(a.q)[at] : zero;
-        *reinterpret_cast<uint4 *>(sm + L::oK + t * L::kPitch + c * 16) = t < n ? reinterpret_cast<const uint4 *>(a.k)[at] : zero;
-    }
-    bool odd = false;                             // something that is not finite may meet a zero
-    for (int i = tid; i < kRows * tiles; i += kThreads) {
-        const int t = i / tiles, c = i - t * tiles;
-        const uint4 y = t < n ? reinterpret_cast<const uint4 *>(a.v)[(((size_t)b * T + t) * a.H + h) * kPieces + c0 / 8 + c] : zero;
-        odd |= !(finite_bf16x2(y.x) && finite_bf16x2(y.y) && finite_bf16x2(y.z) && finite_bf16x2(y.w));
-        *reinterpret_cast<uint4 *>(sm + L::oV + t * L::kPitchV + c * 16) = y;
-    }
-    read_nodes(a, b, h, n, nd, tab, kRows);
-    __syncthreads();
+    read_nodes(a, b, h, n, tid, nd, sync);
     if (tid < 2 * kRows) {                        // a row's norms, thread = row of q or k
         const int t = tid % kRows;
         const bool is_k = tid >= kRows;
@@ -384,7 +390,7 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
         }
         (is_k ? nd->rk_la : nd->rq_la)[t] = kNorm ? rsqrtf(all + a.norm_eps) : 1.f;
     }
-    __syncthreads();
+    sync();
     const uint32_t q_at = tc::smem_u32(sm + L::oQ), k_at = tc::smem_u32(sm + L::oK), v_at = tc::smem_u32(sm + L::oV);
 
     // ---- the tables: a warp has 16 rows, all columns.  What u takes from u goes to shared memory, what the read-out takes
@@ -435,7 +441,7 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
                     float q = qk[0][i][2 * r + x];
                     y[i][x] = G > 1 && sc ? qk[G - 1][i][2 * r + x] : q;
                     if (G > 1) q += qk[G - 1][i][2 * r + x];
-                    const float decay = fold >> j & 1 ? tab[t * kRows + j] * nd->rk_la[j] : 0.f;
+                    const float decay = fold >> j & 1 ? decay_of(nd, t, j) * nd->rk_la[j] : 0.f;
                     w[x] = fold >> j & 1 ? fq * decay * q : 0.f;
                     if (j < t) tab[j * kRows + t] = fold >> j & 1 ? bt * decay * kk[i][2 * r + x] : 0.f;
                     y[i][x] = seen >> j & 1 ? y[i][x] * f * nd->rk_sm[G > 1 ? sc : 0][j] : -INFINITY;
@@ -487,7 +493,7 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
             }
         }
     }
-    __syncthreads();                              // q and k have been read: the right-hand sides and q S0 take their places
+    sync();                                       // k has been read: the right-hand sides take its place
 #pragma unroll
     for (int un = 0; un < kUnits; ++un) {
         const int tile = warp + 4 * un, at = tile * 8 + 2 * c4;
@@ -509,7 +515,7 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
                 }
             }
     }
-    __syncthreads();
+    sync();
     // ---- the substitution: a thread's column, by blocks of 16 nodes.  A node that u_j does not reach has a zero in the table;
     // where u_j is not finite, the paths are asked. ----
     if (tid < cols) {
@@ -558,9 +564,11 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
             for (int i = 0; i < 16; ++i) col[(t0 + i) * cols] = r[i];
         }
     }
-    odd = __syncthreads_or(odd);
+    if (odd) s_odd = 1;
+    sync();
+    odd = s_odd != 0;
     if (a.u)
-        for (int i = tid; i < n * (cols / 4); i += kThreads) {
+        for (int i = tid; i < n * (cols / 4); i += kHalf) {
             const int t = i / (cols / 4), c = (i - t * (cols / 4)) * 4;
             *reinterpret_cast<float4 *>(a.u + (((size_t)b * T + t) * a.H + h) * D + c0 + c) =
                 *reinterpret_cast<const float4 *>(su + t * cols + c);
@@ -596,7 +604,7 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
     }
     // x (hi + lo) of the A fragments, as a table [t][j] in the table's place
     auto dump = [&](const uint32_t (&hi)[kNt / 2][4], const uint32_t (&lo)[kNt / 2][4], bool both) {
-        __syncthreads();
+        sync();
         if (warp < R)
 #pragma unroll
             for (int k = 0; k < kNt / 2; ++k)
@@ -607,12 +615,11 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
                     to[0] = y.x + w.x;
                     to[1] = y.y + w.y;
                 }
-        __syncthreads();
+        sync();
     };
-    float *s_to = odd ? su : st;
     if (odd) {
         dump(bh_f, bl_f, true);
-        for (int i = tid; i < n * cols; i += kThreads) {
+        for (int i = tid; i < n * cols; i += kHalf) {
             const int t = i / cols, c = i - t * cols;
             for (unsigned long long w = (nd->above[t] | 1ull << t) & nd->fold; w; w &= w - 1) {
                 const int j = __ffsll(w) - 1;
@@ -639,39 +646,65 @@ __device__ void tree_part(const Args &a, Sums *sums, uint8_t *sm, Nodes *nd, int
             }
 #pragma unroll
             for (int r = 0; r < 2; ++r)
-                *reinterpret_cast<float2 *>(s_to + (warp * 16 + r * 8 + g4) * cols + tile * 8 + 2 * c4) = make_float2(o[2 * r], o[2 * r + 1]);
+                *reinterpret_cast<float2 *>(st + (warp * 16 + r * 8 + g4) * cols + tile * 8 + 2 * c4) = make_float2(o[2 * r], o[2 * r + 1]);
         }
     }
     if (odd) {
-        __syncthreads();
-        for (int i = tid; i < n * cols; i += kThreads) {
+        sync();
+        for (int i = tid; i < n * cols; i += kHalf) {
             const int t = i / cols, c = i - t * cols;
             for (unsigned long long w = (nd->above[t] | 1ull << t) & nd->keep; w; w &= w - 1) {
                 const int j = __ffsll(w) - 1;
                 const float v = to_f32(*reinterpret_cast<const __nv_bfloat16 *>(sm + L::oV + j * L::kPitchV + c * 2));
-                if (!finite(v)) su[i] += tab[t * kRows + j] * v;
+                if (!finite(v)) st[i] += tab[t * kRows + j] * v;
             }
         }
-        __syncthreads();
-        for (int i = tid; i < n * cols; i += kThreads) st[i] = su[i];
     }
 }
 
 template <int D, int G, bool kNorm, int R>
-__global__ void __launch_bounds__(kThreads, 2) tree_tc_kernel(Args a) {
+__global__ void __launch_bounds__(kThreads, Layout<D, R>::kCtas) tree_tc_kernel(Args a) {
     using L = Layout<D, R>;
     extern __shared__ __align__(128) uint8_t dyn_tc[];
-    __shared__ Nodes nodes;
-    const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, n = nodes_of(a, b);
-    Sums *sums = reinterpret_cast<Sums *>(dyn_tc);
-    if (n > 0) {                                  // (the same for the whole cluster)
-        cache_part<D, G, kNorm, R>(a, sums, dyn_tc, b, h, n, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
-        tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank);
-    } else if (threadIdx.x == 0 && a.n_nodes && a.n_nodes[b] != n) {
-        atomicMin(a.status, (int)NATSL_ERR_TREE);
+    __shared__ typename L::N nodes;
+    const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, tid = threadIdx.x;
+    const int n = nodes_of(a, b), cols = D / a.cluster;
+    const Stream<D, R> in(a, dyn_tc, bh, tid, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
+    typename L::S *sums = reinterpret_cast<typename L::S *>(dyn_tc);
+    if (tid < kHalf)
+#pragma unroll
+        for (int u = 0; u < L::kSlots - 1; ++u) in.fetch(u);
+    // q, k and the columns of v
+    constexpr int kPieces = L::kRowBytes / 16, kLoads = (L::kRows * kPieces + kThreads - 1) / kThreads;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    uint4 x[2][kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int e = tid + i * kThreads, t = e / kPieces;
+        const size_t at = (((size_t)b * a.T + t) * a.H + h) * kPieces + e - t * kPieces;
+        x[0][i] = t < n ? reinterpret_cast<const uint4 *>(a.q)[at] : zero;
+        x[1][i] = t < n ? reinterpret_cast<const uint4 *>(a.k)[at] : zero;
     }
-    join_rows<__nv_bfloat16, D>(a, b, h, n, rank, sums, reinterpret_cast<const float *>(dyn_tc + L::oAcc), L::kAccPitch,
-                                reinterpret_cast<const float *>(dyn_tc + L::oK), reinterpret_cast<const float *>(dyn_tc + L::oTab));
+    bool odd = false;                             // something that is not finite may meet a zero
+    for (int e = tid; e < L::kRows * (cols / 8); e += kThreads) {
+        const int t = e / (cols / 8), c = e - t * (cols / 8);
+        const uint4 y = t < n ? reinterpret_cast<const uint4 *>(a.v)[(((size_t)b * a.T + t) * a.H + h) * kPieces + rank * cols / 8 + c] : zero;
+        odd |= !(finite_bf16x2(y.x) && finite_bf16x2(y.y) && finite_bf16x2(y.z) && finite_bf16x2(y.w));
+        *reinterpret_cast<uint4 *>(dyn_tc + L::oV + t * L::kPitchV + c * 16) = y;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int e = tid + i * kThreads, t = e / kPieces, c = e - t * kPieces;
+        if (t < L::kRows) {
+            *reinterpret_cast<uint4 *>(dyn_tc + L::oQ + t * L::kPitch + c * 16) = x[0][i];
+            *reinterpret_cast<uint4 *>(dyn_tc + L::oK + t * L::kPitch + c * 16) = x[1][i];
+        }
+    }
+    odd = __syncthreads_or(odd);
+    if (tid < kHalf) cache_part<D, G, kNorm, R>(a, sums, dyn_tc, in, n);
+    else tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank, odd);
+    join_rows<__nv_bfloat16, D>(a, b, h, n, rank, sums, reinterpret_cast<const float *>(dyn_tc + L::oRing), L::kAccPitch,
+                                reinterpret_cast<const float *>(dyn_tc + L::oO), reinterpret_cast<const float *>(dyn_tc + L::oT));
 }
 
 template <int D, int G, bool kNorm, int R>
@@ -679,7 +712,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     auto kernel = tree_tc_kernel<D, G, kNorm, R>;
     cudaError_t e = allow_smem(kernel, Layout<D, R>::kTotal);
     if (e != cudaSuccess) return e;
-    return launch_clusters(kernel, a, BH, Layout<D, R>::kTotal, st);
+    return launch_clusters(kernel, a, BH, kThreads, Layout<D, R>::kTotal, st);
 }
 template <int D, int G, bool kNorm>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
