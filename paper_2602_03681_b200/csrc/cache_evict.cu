@@ -4,9 +4,9 @@
 //   weight_j += sum_t sum_s exp(scale q_ts.k_js - lse_ts)   over the rows that see it,
 // from the log-sum-exps that the attention itself has left, so K is read once and V not at all.
 //
-// natsl_cache_evict keeps the first entries, the latest ones and the heaviest of the rest.  Two kernels: one selects (a
-// radix select of the threshold on the weights' bits, ties to the lowest index) and lists the entries that stay; one
-// moves them to the front, in order and in place.
+// natsl_cache_evict keeps the first entries, the latest ones and the heaviest of the rest (a bisection on the weights'
+// bits finds the threshold; ties to the lowest index) and moves them to the front, in order and in place.
+#include <algorithm>
 #include "common.cuh"
 #include "natsl_internal.h"
 #include "tc_common.cuh"
@@ -15,6 +15,22 @@ namespace natsl {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+
+// 16 bytes global -> shared past the registers
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ float square_sum(uint32_t bf16x2, float s) {
+    const float lo = __uint_as_float(bf16x2 << 16), hi = __uint_as_float(bf16x2 & 0xffff0000u);
+    return fmaf(lo, lo, fmaf(hi, hi, s));
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 
 // ------------------------------------------------------------------------------------------
 // Weights, fp32 CUDA cores: eight lanes share a key, each with D / 8 neighbouring columns; the query rows pass through
@@ -89,148 +105,337 @@ cache_weights_simt_kernel(const ST *__restrict__ q, const float *__restrict__ ls
 }
 
 // ------------------------------------------------------------------------------------------
-// Eviction: selection
+// Weights, tensor cores (bf16 storage, one or two softmax heads per linear head).  Bound by reading K once, up to some 64
+// rows.  A CTA takes a run of a pair's keys through a ring of asynchronous copies, tiles of 64, and up to 64 rows of q at a
+// time as fragments in registers (R: 16-row tiles); its warps share the tile by keys, beyond 32 rows also by rows.
 // ------------------------------------------------------------------------------------------
-constexpr int kSThreads = 1024, kBins = 2048;
+constexpr int kTTile = 64, kTStages = 3, kMaxRun = 1024;
 
-// Weights in the order of unsigned words: a NaN below everything, both zeros equal.
+template <int D, int G, bool kNorm, int R>
+__global__ void __launch_bounds__(kWThreads, R == 1 ? 4 : 3)
+cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__ lse, const int32_t *__restrict__ visible,
+                        const uint8_t *__restrict__ k_cache, const int32_t *__restrict__ cache_len, int cap,
+                        float *__restrict__ weight, int H, int T, float scale, float norm_eps, int runs, int run) {
+    constexpr int ds = D / G, kKs = ds / 16, kRows = 16 * R, kMt = R < 2 ? R : 2, kRowGroups = R / kMt, kKeyGroups = 4 / kRowGroups;
+    constexpr int kKeys = kTTile / kKeyGroups, kNt = kKeys / 8, kRowBytes = D * 2, kPieces = kRowBytes / 16, kStep = kWThreads / kPieces;
+    constexpr int kTileBytes = kTTile * kRowBytes;
+    extern __shared__ __align__(128) uint8_t dyn_w[];      // the ring; then the sums [row groups][run]
+    __shared__ float2 s_row[G][kRows];            // factor to base-2 logits, log-sum-exp in base 2
+    __shared__ int s_vis[G][kRows];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
+    const int rg = warp / kKeyGroups, kg = warp - rg * kKeyGroups, r0 = rg * 16 * kMt;
+    const int bh = blockIdx.x / runs, b = bh / H, h = bh - b * H, n = min(max(cache_len[bh], 0), cap);
+    const int from = (blockIdx.x - bh * runs) * run, to = min(n, from + run), tiles = (to - from + kTTile - 1) / kTTile;
+    if (from >= n) return;
+    float *s_sum = reinterpret_cast<float *>(dyn_w + kTStages * kTileBytes);
+    const uint32_t ring = tc::smem_u32(dyn_w);
+    const int piece = tid % kPieces, row0 = tid / kPieces;
+    const uint8_t *kc = k_cache + ((size_t)bh * cap + from) * kRowBytes + piece * 16;
+    const uint32_t dst0 = row0 * kRowBytes + ((piece ^ (row0 & 7)) << 4);
+    auto fetch = [&](int t) {
+        if (t < tiles) {
+#pragma unroll
+            for (int i = 0; i < kTTile / kStep; ++i) {
+                const int j = t * kTTile + row0 + i * kStep;
+                cp_async16(ring + t % kTStages * kTileBytes + dst0 + i * kStep * kRowBytes,
+                           kc + (size_t)min(j, to - from - 1) * kRowBytes);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int t0 = 0; t0 < T; t0 += kRows) {
+        const int rows = min(kRows, T - t0);
+        if (t0) __syncthreads();                  // (the last tiles and rows have been read)
+#pragma unroll
+        for (int i = 0; i < kTStages - 1; ++i) fetch(i);
+        for (int e = tid; e < kRows * G; e += kWThreads) {
+            const int g = e / kRows, t = e - g * kRows;
+            int vis = 0;
+            float l = 0.f;
+            if (t < rows) {
+                l = lse[((size_t)bh * G + g) * T + t0 + t];
+                vis = visible ? max(min(visible[((size_t)b * T + t0 + t) * H + h], n), 0) : n;
+                if (!isfinite(l)) vis = 0;        // (a row that sees nothing)
+            }
+            s_vis[g][t] = vis - from;
+            s_row[g][t] = make_float2(scale * kLog2e, l * kLog2e);
+        }
+        // (q passes through the ring's last place, which the first tile's turn fills)
+        constexpr int kQ = (kTStages - 1) * kTileBytes;
+        for (int e = tid; e < kRows * kPieces; e += kWThreads) {
+            const int t = e / kPieces, c = e - t * kPieces;
+            *reinterpret_cast<uint4 *>(dyn_w + kQ + t * kRowBytes + ((c ^ (t & 7)) << 4)) =
+                t < rows ? *reinterpret_cast<const uint4 *>(q + (((size_t)b * T + t0 + t) * H + h) * kRowBytes + c * 16) : make_uint4(0, 0, 0, 0);
+        }
+        __syncthreads();
+        uint32_t qf[kMt][D / 16][4];
+#pragma unroll
+        for (int m = 0; m < kMt; ++m)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const int t = r0 + m * 16 + (lane & 15);
+                tc::ldmatrix_x4(ring + kQ + t * kRowBytes + (((2 * k + (lane >> 4)) ^ (t & 7)) << 4), qf[m][k]);
+            }
+        float2 f[G][kMt][2];
+        int vis[G][kMt][2];
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    f[g][m][r] = s_row[g][r0 + m * 16 + r * 8 + g4];
+                    vis[g][m][r] = s_vis[g][r0 + m * 16 + r * 8 + g4] - kg * kKeys - 2 * c4;
+                    if (kNorm) {
+                        float ss = 0.f;
+#pragma unroll
+                        for (int k = g * kKs; k < (g + 1) * kKs; ++k)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) ss = square_sum(qf[m][k][r + 2 * x], ss);
+                        ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+                        ss += __shfl_xor_sync(0xffffffffu, ss, 2);
+                        f[g][m][r].x *= rsqrtf(ss / ds + norm_eps);
+                    }
+                }
+        for (int t = 0; t < tiles; ++t) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kTStages - 2) : "memory");
+            __syncthreads();                      // tile t is there, and every warp is done with tile t - 1 ...
+            fetch(t + kTStages - 1);              // ... whose place this one takes
+            const uint32_t kt = ring + t % kTStages * kTileBytes;
+            float sum[kNt][2];
+#pragma unroll
+            for (int i = 0; i < kNt; ++i) sum[i][0] = sum[i][1] = 0.f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                float x[kMt][kNt][4], kk[kNt];
+#pragma unroll
+                for (int i = 0; i < kNt; ++i) {
+                    kk[i] = 0.f;
+#pragma unroll
+                    for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) x[m][i][y] = 0.f;
+                }
+#pragma unroll
+                for (int k = g * kKs; k < (g + 1) * kKs; ++k)
+#pragma unroll
+                    for (int i = 0; i < kNt; i += 2) {
+                        const int row = kg * kKeys + i * 8 + (lane & 7) + (lane >> 4) * 8;
+                        uint32_t bf[4];
+                        tc::ldmatrix_x4(kt + row * kRowBytes + (((2 * k + ((lane >> 3) & 1)) ^ (row & 7)) << 4), bf);
+#pragma unroll
+                        for (int m = 0; m < kMt; ++m) {
+                            mma_bf16(x[m][i], qf[m][k], bf[0], bf[1]);
+                            mma_bf16(x[m][i + 1], qf[m][k], bf[2], bf[3]);
+                        }
+                        if (kNorm) {
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) kk[i + y / 2] = square_sum(bf[y], kk[i + y / 2]);
+                        }
+                    }
+#pragma unroll
+                for (int i = 0; i < kNt; ++i) {
+                    float w[2] = {1.f, 1.f};
+                    if (kNorm) {                  // (a lane's sum of squares belongs to key g4 of tile i, its columns to 2 c4, + 1)
+                        kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 1);
+                        kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 2);
+                        const float y = rsqrtf(fmaf(kk[i], 1.f / ds, norm_eps));
+                        w[0] = __shfl_sync(0xffffffffu, y, c4 * 8);
+                        w[1] = __shfl_sync(0xffffffffu, y, c4 * 8 + 4);
+                    }
+#pragma unroll
+                    for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                const float z = kNorm ? x[m][i][2 * r + y] * w[y] : x[m][i][2 * r + y];
+                                const float e = tc::ex2_ftz(fmaf(z, f[g][m][r].x, -f[g][m][r].y));
+                                sum[i][y] += t * kTTile + i * 8 + y < vis[g][m][r] ? e : 0.f;
+                            }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kNt; ++i)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) sum[i][y] += __shfl_xor_sync(0xffffffffu, sum[i][y], o);
+                }
+            if (g4 == 0) {                        // (a key's sums always belong to the same warp of a row group)
+#pragma unroll
+                for (int i = 0; i < kNt; ++i) {
+                    float2 *at = reinterpret_cast<float2 *>(s_sum + rg * run + t * kTTile + kg * kKeys + i * 8 + 2 * c4);
+                    const float2 was = t0 ? *at : make_float2(0.f, 0.f);
+                    *at = make_float2(was.x + sum[i][0], was.y + sum[i][1]);
+                }
+            }
+        }
+        cp_async_wait_all();
+    }
+    __syncthreads();
+    for (int j = tid; j < to - from; j += kWThreads) {
+        float z = s_sum[j];
+        if (kRowGroups > 1) z += s_sum[run + j];
+        weight[(size_t)bh * cap + from + j] += z;
+    }
+}
+
+template <int D, int G, bool kNorm, int R>
+cudaError_t launch_weights_tc(const void *q, const float *lse, const int32_t *visible, const void *k_cache, const int32_t *cache_len,
+                              int cap, float *weight, float scale, Shape s, float norm_eps, cudaStream_t st) {
+    // Runs of 128 to 1024 keys: as short as one resident set of CTAs allows.
+    const long long BH = (long long)s.B * s.H, resident = 148 * (R == 1 ? 4 : 3), per = (BH * cap + resident - 1) / resident;
+    const int run = (int)std::min<long long>(kMaxRun, std::max<long long>(128, (per + kTTile - 1) / kTTile * kTTile));
+    const int runs = (cap + run - 1) / run, ring = kTStages * kTTile * D * 2;
+    auto kernel = cache_weights_tc_kernel<D, G, kNorm, R>;
+    cudaError_t e = allow_smem(kernel, ring + 2 * kMaxRun * 4);
+    if (e != cudaSuccess) return e;
+    kernel<<<(int)BH * runs, kWThreads, ring + (R > 2 ? 2 : 1) * run * 4, st>>>(
+        (const uint8_t *)q, lse, visible, (const uint8_t *)k_cache, cache_len, cap, weight, s.H, s.L, scale, norm_eps, runs, run);
+    count_launch();
+    return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------
+// Eviction.  Every CTA of a pair's cluster finds out what stays (all of them the same: that costs no time, and nobody waits for
+// a list), then they move the rows in waves: a wave of rows is read into shared memory by the CTAs, and written behind the
+// cluster's barrier.  Entry r comes from kept[r] >= r, so what a wave writes lies below everything that later waves read.  And
+// once one entry is gone all behind it move: what lies before the first gap is left in place.
+// ------------------------------------------------------------------------------------------
+constexpr int kEThreads = 512, kEWarps = kEThreads / 32;
+
+// Weights in the order of unsigned words: a NaN below everything (0), both zeros equal.
 __device__ __forceinline__ uint32_t order_key(float w) {
     if (isnan(w)) return 0u;
     const uint32_t x = __float_as_uint(w + 0.f);
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kSThreads)
-evict_select_kernel(const float *__restrict__ weight, int32_t *__restrict__ cache_len, int cap, int keep, int first, int recent,
-                    int32_t *__restrict__ kept) {
-    __shared__ int hist[kBins], s_warp[2][32], s_pick[2];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x;
-    const float *w = weight + (size_t)bh * cap;
+// kHeld: entries per lane whose keys stay in registers (512 kHeld per pair); more lie in shared memory where the rows will be,
+// and what does not fit there is read again.
+template <int kRowBytes, int kHeld>
+__global__ void __launch_bounds__(kEThreads)
+evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first, int recent,
+             int32_t *kept, int cluster, int rows) {
+    extern __shared__ __align__(16) uint8_t dyn_e[];       // [2][rows][kRowBytes], then the rows' weights and sources
+    __shared__ int s_warp[2][kEWarps], s_count[2][kEWarps], s_gap;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x / cluster, rank = blockIdx.x - bh * cluster;
+    float *w = weight + (size_t)bh * cap;
     int32_t *list = kept + (size_t)bh * keep;
     const int n = min(max(cache_len[bh], 0), cap);
-    if (n <= keep) {
-        for (int i = tid; i < n; i += kSThreads) list[i] = i;
+    if (n <= keep) {                              // (the same for the whole cluster)
+        for (int i = rank * kEThreads + tid; i < n; i += cluster * kEThreads) list[i] = i;
         return;
     }
-    // the threshold: the weight of rank `need` among the entries that are not safe anyway, from its high bits down
-    const int lo = first, hi = n - recent;
-    int need = keep - first - recent;             // (entries still to be taken with the bits found so far)
-    uint32_t prefix = 0;
-    for (int pass = 0; pass < 3 && need > 0; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, above = shift + bits;
-        for (int i = tid; i < kBins; i += kSThreads) hist[i] = 0;
-        __syncthreads();
-        for (int j = lo + tid; j < hi; j += kSThreads) {
-            const uint32_t x = order_key(w[j]);
-            if (pass == 0 || x >> above == prefix) atomicAdd(&hist[x >> shift & ((1u << bits) - 1u)], 1);
-        }
-        __syncthreads();
-        // thread i holds bins 2 i, 2 i + 1, counted from the top
-        const int c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
-        int sum = c0 + c1;
+    // ---- a warp owns a run of entries, a lane every 32nd of them.  Candidates have their key; what is safe anyway, or no entry,
+    // has 0, which no count below takes in. ----
+    const int lo = first, hi = n - recent, want = keep - first - recent;      // candidates; how many of them stay
+    const int run = ((n + kEWarps - 1) / kEWarps + 31) / 32 * 32, j0 = min(n, warp * run), j1 = min(n, j0 + run), steps = (j1 - j0 + 31) / 32;
+    auto is_candidate = [&](int j) { return (j < j1) & (j >= lo) & (j < hi); };
+    auto key_of = [&](int j) { return is_candidate(j) ? order_key(w[j]) : 0u; };
+    uint32_t held[kHeld];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += y;
-        }
-        if (lane == 31) s_warp[0][warp] = sum;
-        __syncthreads();
-        if (warp == 0) {
-            int x = s_warp[0][lane];
+    for (int i = 0; i < kHeld; ++i) held[i] = key_of(j0 + i * 32 + lane);
+    const int room = rows * (2 * kRowBytes + 8) / (kEWarps * 128), spare = max(0, min(steps - kHeld, room));
+    uint32_t *more = reinterpret_cast<uint32_t *>(dyn_e) + warp * room * 32 + lane;
+    for (int i = 0; i < spare; ++i) more[i * 32] = key_of(j0 + (kHeld + i) * 32 + lane);
+    auto each = [&](auto &&f) {                   // f(entry, its key), the warp together
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            s_warp[0][lane] = x;
-        }
-        __syncthreads();
-        const int upto = sum + (warp ? s_warp[0][warp - 1] : 0), before = upto - c0 - c1;
-        if (before < need && need <= upto) {
-            const bool second = need > before + c0;
-            s_pick[0] = kBins - 1 - 2 * tid - second;
-            s_pick[1] = need - before - (second ? c0 : 0);
-        }
-        __syncthreads();
-        prefix = prefix << bits | (uint32_t)s_pick[0];
-        need = s_pick[1];
-        __syncthreads();
-    }
-    // prefix: the threshold; need: how many of its equals stay.  Warps own runs of entries: count, scan, list.
-    const bool none = keep - first - recent <= 0;
-    const int run = ((n + 31) / 32 + 31) / 32 * 32, j0 = min(n, warp * run), j1 = min(n, j0 + run);
-    auto look = [&](int j, bool &over, bool &equal) {
-        over = j < n && (j < lo || j >= hi);
-        equal = false;
-        if (!over && j < n && !none) {
-            const uint32_t x = order_key(w[j]);
-            over = x > prefix;
-            equal = x == prefix;
+        for (int i = 0; i < kHeld; ++i) f(j0 + i * 32 + lane, held[i]);
+        for (int i = kHeld; i < steps; ++i) {
+            const int j = j0 + i * 32 + lane;
+            f(j, i < kHeld + spare ? more[(i - kHeld) * 32] : key_of(j));
         }
     };
-    int overs = 0, equals = 0;
-    for (int j = j0; j < j1; j += 32) {
-        bool o, e;
-        look(j + lane, o, e);
-        overs += __popc(__ballot_sync(0xffffffffu, o));
-        equals += __popc(__ballot_sync(0xffffffffu, e));
+    // ---- the threshold, bit by bit from the highest in which two candidates differ: is what has it set enough?  (Histograms of
+    // the leading bits meet in a few bins: 57 us a call at 16 pairs of 8192.) ----
+    int need = 0;
+    uint32_t prefix = 0xffffffffu;                // (nothing is over it or equal to it where nothing more is wanted)
+    if (want > 0) {
+        uint32_t all = 0xffffffffu, any = 0u;
+        each([&](int j, uint32_t x) {
+            all &= is_candidate(j) ? x : 0xffffffffu;
+            any |= x;
+        });
+        all = __reduce_and_sync(0xffffffffu, all);
+        any = __reduce_or_sync(0xffffffffu, any);
+        if (lane == 0) { s_warp[0][warp] = (int)all; s_warp[1][warp] = (int)any; }
+        __syncthreads();
+        all = __reduce_and_sync(0xffffffffu, (uint32_t)s_warp[0][lane % kEWarps]);
+        any = __reduce_or_sync(0xffffffffu, (uint32_t)s_warp[1][lane % kEWarps]);
+        const int top = 31 - __clz((int)(all ^ any));                          // (-1: all alike)
+        prefix = top < 0 ? all : top == 31 ? 0u : all & ~((2u << top) - 1u);
+        auto count = [&](uint32_t x0, int set) {  // candidates with keys >= x0 > 0; two sets of counts: one barrier a count
+            int c = 0;
+            each([&](int, uint32_t x) { c += x >= x0; });
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (lane == 0) s_count[set][warp] = c;
+            __syncthreads();
+            return __reduce_add_sync(0xffffffffu, lane < kEWarps ? s_count[set][lane] : 0);
+        };
+        for (int bit = top; bit >= 0; --bit)
+            if (count(prefix | 1u << bit, bit & 1) >= want) prefix |= 1u << bit;
+        need = want;
+        if (prefix != 0xffffffffu) {              // (uniform)
+            __syncthreads();
+            need -= count(prefix + 1u, 0);
+        }
     }
-    if (lane == 0) { s_warp[0][warp] = overs; s_warp[1][warp] = equals; }
+    // prefix: the threshold; need: how many of its equals stay, the lowest
+    auto over = [&](int j, uint32_t x) { return (j < j1) & ((j < lo) | (j >= hi) | (x > prefix)); };
+    auto equal = [&](int j, uint32_t x) { return is_candidate(j) & (x == prefix) & (want > 0); };
+    int overs = 0, equals = 0;
+    each([&](int j, uint32_t x) {
+        overs += over(j, x);
+        equals += equal(j, x);
+    });
+    overs = __reduce_add_sync(0xffffffffu, overs);
+    equals = __reduce_add_sync(0xffffffffu, equals);
     __syncthreads();
-    int at_over = 0, at_equal = 0;
-    for (int i = 0; i < warp; ++i) { at_over += s_warp[0][i]; at_equal += s_warp[1][i]; }
-    for (int j = j0; j < j1; j += 32) {
-        bool o, e;
-        look(j + lane, o, e);
+    if (lane == 0) { s_warp[0][warp] = overs; s_warp[1][warp] = equals; }
+    if (tid == 0) s_gap = keep;
+    __syncthreads();
+    // ---- the list: entry j goes to the number of overs below it and of the equals that stay.  The first gap is the first place
+    // whose entry comes from behind it.  (Each CTA writes the whole list, the same; it then reads its own.) ----
+    int at_over = __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[0][lane] : 0);
+    int at_equal = __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[1][lane] : 0);
+    int gap = keep;
+    each([&](int j, uint32_t x) {
+        const bool o = over(j, x), e = equal(j, x);
         const unsigned mo = __ballot_sync(0xffffffffu, o), me = __ballot_sync(0xffffffffu, e), below = (1u << lane) - 1u;
-        const int eq = at_equal + __popc(me & below), ov = at_over + __popc(mo & below);
-        if (o || (e && eq < need)) list[ov + min(eq, need)] = j + lane;
+        const int eq = at_equal + __popc(me & below), to = at_over + __popc(mo & below) + min(eq, need);
         at_over += __popc(mo);
         at_equal += __popc(me);
-    }
-    if (tid == 0) cache_len[bh] = keep;           // (every thread has read the old length: barriers above)
-}
-
-// ------------------------------------------------------------------------------------------
-// Eviction: the move.  Entry r comes from kept[r] >= r.  A wave of rows is read into shared memory by the CTAs of a pair
-// (a cluster), and written after the cluster's barrier.  What a wave writes lies below everything that later waves read:
-// their sources are no lower than their own places.
-// ------------------------------------------------------------------------------------------
-constexpr int kMThreads = 256;
-
-__device__ __forceinline__ void cp_async16(void *dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-template <int kRowBytes, int kRows>
-__global__ void __launch_bounds__(kMThreads)
-evict_move_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, const int32_t *__restrict__ cache_len,
-                  const int32_t *__restrict__ kept, int cap, int keep, int cluster) {
-    extern __shared__ __align__(16) uint8_t rows[];   // [2][kRows][kRowBytes]
-    constexpr int kPieces = kRowBytes / 16;
-    const int tid = threadIdx.x, bh = blockIdx.x / cluster, rank = blockIdx.x - bh * cluster;
-    const int n = min(max(cache_len[bh], 0), keep);
-    const int32_t *list = kept + (size_t)bh * keep;
-    uint8_t *kc = k_cache + (size_t)bh * cap * kRowBytes, *vc = v_cache + (size_t)bh * cap * kRowBytes;
-    float *w = weight + (size_t)bh * cap;
-    const int wave = cluster * kRows;
-    for (int r0 = 0; r0 < n; r0 += wave) {        // (every CTA of the cluster: the same number of barriers)
-        const int mine = r0 + rank * kRows;
-        float x = 0.f;
-        bool move = false;
-        if (tid < kRows && mine + tid < n) {
-            const int src = list[mine + tid];
-            move = src != mine + tid;
-            if (move) x = w[src];
+        if (o | (e & (eq < need))) {
+            list[to] = j;
+            gap = to < j ? min(gap, to) : gap;
         }
-        for (int i = tid; i < kRows * kPieces; i += kMThreads) {
+    });
+    gap = __reduce_min_sync(0xffffffffu, gap);
+    if (lane == 0 && gap < keep) atomicMin(&s_gap, gap);
+    __syncthreads();
+    gap = s_gap;
+    const int wave = cluster * rows;
+    // ---- the move ----
+    constexpr int kPieces = kRowBytes / 16;
+    float *s_w = reinterpret_cast<float *>(dyn_e + 2 * rows * kRowBytes);
+    int *s_from = reinterpret_cast<int *>(s_w + rows);
+    const uint32_t buffer = tc::smem_u32(dyn_e);
+    uint8_t *kc = k_cache + (size_t)bh * cap * kRowBytes, *vc = v_cache + (size_t)bh * cap * kRowBytes;
+    for (int r0 = gap; r0 < keep || r0 == gap; r0 += wave) {   // (once at least; every CTA of the cluster as often)
+        const int to = r0 + rank * rows, count = max(0, min(rows, keep - to));
+        for (int r = tid; r < count; r += kEThreads) {
+            const int src = list[to + r];
+            s_from[r] = src;
+            s_w[r] = w[src];
+        }
+        __syncthreads();
+        for (int i = tid; i < count * kPieces; i += kEThreads) {
             const int r = i / kPieces, c = i - r * kPieces;
-            if (mine + r >= n) break;
-            const int src = list[mine + r];
-            if (src == mine + r) continue;
-            cp_async16(rows + i * 16, kc + (size_t)src * kRowBytes + c * 16);
-            cp_async16(rows + (kRows * kPieces + i) * 16, vc + (size_t)src * kRowBytes + c * 16);
+            const size_t at = (size_t)s_from[r] * kRowBytes + c * 16;
+            cp_async16(buffer + i * 16, kc + at);
+            cp_async16(buffer + (rows * kPieces + i) * 16, vc + at);
         }
         cp_async_wait_all();
         if (cluster > 1) {
@@ -238,32 +443,32 @@ evict_move_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, const int32
         } else {
             __syncthreads();
         }
-        if (move) w[mine + tid] = x;
-        for (int i = tid; i < kRows * kPieces; i += kMThreads) {
-            const int r = i / kPieces, c = i - r * kPieces;
-            if (mine + r >= n) break;
-            if (list[mine + r] == mine + r) continue;
-            *reinterpret_cast<uint4 *>(kc + (size_t)(mine + r) * kRowBytes + c * 16) = *reinterpret_cast<const uint4 *>(rows + i * 16);
-            *reinterpret_cast<uint4 *>(vc + (size_t)(mine + r) * kRowBytes + c * 16) =
-                *reinterpret_cast<const uint4 *>(rows + (kRows * kPieces + i) * 16);
+        for (int r = tid; r < count; r += kEThreads) w[to + r] = s_w[r];
+        for (int i = tid; i < count * kPieces; i += kEThreads) {
+            const size_t at = (size_t)to * kRowBytes + i * 16;
+            *reinterpret_cast<uint4 *>(kc + at) = *reinterpret_cast<const uint4 *>(dyn_e + i * 16);
+            *reinterpret_cast<uint4 *>(vc + at) = *reinterpret_cast<const uint4 *>(dyn_e + (rows * kPieces + i) * 16);
         }
-        __syncthreads();                          // (the next wave fills the same rows)
+        if (r0 == gap && rank == 0 && tid == 0) cache_len[bh] = keep;     // (behind the barrier: everyone has read the old one)
+        __syncthreads();                          // (the next wave fills the same places)
     }
 }
 
 template <int kRowBytes>
-cudaError_t launch_move(void *k_cache, void *v_cache, float *weight, const int32_t *cache_len, const int32_t *kept, int cap,
-                        int keep, int BH, cudaStream_t st) {
-    constexpr int kRows = 32 * 1024 / kRowBytes;  // 64 KB of rows per CTA and wave
-    auto kernel = evict_move_kernel<kRowBytes, kRows>;
-    cudaError_t e = allow_smem(kernel, 2 * kRows * kRowBytes);
+cudaError_t launch_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first, int recent,
+                         int32_t *kept, int BH, cudaStream_t st) {
+    // Few pairs: a cluster for each, two CTAs per multiprocessor (with 192 KB of rows, one, the sixteenth cluster of eight waits
+    // for another's end); many: four.
+    int cluster = 1;
+    while (cluster < 8 && BH * cluster * 2 <= sm_count()) cluster *= 2;
+    const int rows = (cluster > 1 ? 104 : 48) * 1024 / (2 * kRowBytes + 8), bytes = rows * (2 * kRowBytes + 8);
+    auto kernel = cap <= 2048 ? evict_kernel<kRowBytes, 4> : evict_kernel<kRowBytes, 16>;
+    cudaError_t e = allow_smem(kernel, 104 * 1024);
     if (e != cudaSuccess) return e;
-    int cluster = 1;                              // few pairs: as many CTAs for each as the machine has room for
-    while (cluster < 8 && BH * cluster * 2 <= 2 * sm_count() && cluster * kRows < keep) cluster *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(BH * cluster);
-    cfg.blockDim = dim3(kMThreads);
-    cfg.dynamicSmemBytes = 2 * kRows * kRowBytes;
+    cfg.blockDim = dim3(kEThreads);
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -271,7 +476,8 @@ cudaError_t launch_move(void *k_cache, void *v_cache, float *weight, const int32
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, (uint8_t *)k_cache, (uint8_t *)v_cache, weight, cache_len, kept, cap, keep, cluster);
+    e = cudaLaunchKernelEx(&cfg, kernel, (uint8_t *)k_cache, (uint8_t *)v_cache, weight, cache_len, cap, keep, first,
+                           recent, kept, cluster, rows);
     count_launch();
     return e;
 }
@@ -281,6 +487,21 @@ cudaError_t launch_move(void *k_cache, void *v_cache, float *weight, const int32
 cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
                                  const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg,
                                  bool tensor_cores, cudaStream_t st) {
+    if (tensor_cores && hg.G <= 2) {
+#define ARGS q, lse, visible, k_cache, cache_len, cap, weight, scale, s, hg.norm_eps, st
+#define BY_ROWS(D, G, N)                                                                                                   \
+    return s.L <= 16 ? launch_weights_tc<D, G, N, 1>(ARGS) : s.L <= 32 ? launch_weights_tc<D, G, N, 2>(ARGS) : launch_weights_tc<D, G, N, 4>(ARGS)
+#define BY_NORM(D, G) do { if (hg.norm_eps >= 0.f) BY_ROWS(D, G, true); BY_ROWS(D, G, false); } while (0)
+        if (s.d == 128) {
+            if (hg.G == 2) BY_NORM(128, 2);
+            BY_NORM(128, 1);
+        }
+        if (hg.G == 2) BY_NORM(64, 2);
+        BY_NORM(64, 1);
+#undef BY_NORM
+#undef BY_ROWS
+#undef ARGS
+    }
     const int blocks = (cap + kWKeys - 1) / kWKeys;
 #define RUN(ST, D)                                                                                                   \
     cache_weights_simt_kernel<ST, D><<<s.B * s.H * blocks, kWThreads, 0, st>>>((const ST *)q, lse, visible, (const ST *)k_cache, \
@@ -301,13 +522,9 @@ cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t 
 cudaError_t launch_cache_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first,
                                int recent, int32_t *kept, Shape s, cudaStream_t st) {
     const int BH = s.B * s.H, row = s.d * (s.bf16 ? 2 : 4);
-    evict_select_kernel<<<BH, kSThreads, 0, st>>>(weight, cache_len, cap, keep, first, recent, kept);
-    count_launch();
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    if (row == 512) return launch_move<512>(k_cache, v_cache, weight, cache_len, kept, cap, keep, BH, st);
-    if (row == 256) return launch_move<256>(k_cache, v_cache, weight, cache_len, kept, cap, keep, BH, st);
-    return launch_move<128>(k_cache, v_cache, weight, cache_len, kept, cap, keep, BH, st);
+#define ARGS k_cache, v_cache, weight, cache_len, cap, keep, first, recent, kept, BH, st
+    return row == 512 ? launch_evict<512>(ARGS) : row == 256 ? launch_evict<256>(ARGS) : launch_evict<128>(ARGS);
+#undef ARGS
 }
 
 }  // namespace natsl

@@ -3,8 +3,8 @@
 // the tree step has left u, so the tokens do not depend on each other and no product with the state is needed.
 // K/V rows of the retained tokens are appended to the cache.
 //
-// Bound by the state's round trip (8 d^2 bytes per pair): one CTA per pair, every thread's share of the state in flight
-// before the path is read.
+// Bound by the state's round trip (8 d^2 bytes per pair).  One CTA per pair, four per multiprocessor: a thread has four columns
+// and kRows neighbouring rows, read before the path is, four rows at a time afterwards.
 #include "tree_common.cuh"
 
 namespace natsl {
@@ -12,16 +12,40 @@ namespace {
 
 using namespace tree;
 
-constexpr int kCommitThreads = 512;
+constexpr int kCommitThreads = 256;
+
+// V neighbouring elements of a row.
+template <typename ST, int V> struct RowPiece;
+template <> struct RowPiece<float, 4> { using type = uint4; };
+template <> struct RowPiece<float, 2> { using type = uint2; };
+template <> struct RowPiece<__nv_bfloat16, 4> { using type = uint2; };
+template <> struct RowPiece<__nv_bfloat16, 2> { using type = uint32_t; };
+template <int V> __device__ __forceinline__ void unpack(uint4 y, float (&x)[V]) {
+    x[0] = __uint_as_float(y.x); x[1] = __uint_as_float(y.y); x[2] = __uint_as_float(y.z); x[3] = __uint_as_float(y.w);
+}
+template <int V> __device__ __forceinline__ void unpack(uint32_t y, float (&x)[V]) {
+    x[0] = __uint_as_float(y << 16);
+    x[1] = __uint_as_float(y & 0xffff0000u);
+}
+template <int V> __device__ __forceinline__ void unpack(uint2 y, float (&x)[V]) {
+    if constexpr (V == 2) {                       // two fp32
+        x[0] = __uint_as_float(y.x);
+        x[1] = __uint_as_float(y.y);
+    } else {                                      // four bf16
+        x[0] = __uint_as_float(y.x << 16); x[1] = __uint_as_float(y.x & 0xffff0000u);
+        x[2] = __uint_as_float(y.y << 16); x[3] = __uint_as_float(y.y & 0xffff0000u);
+    }
+}
 
 template <typename ST, int D>
-__global__ void __launch_bounds__(kCommitThreads)
+__global__ void __launch_bounds__(kCommitThreads, 4)
 tree_commit_kernel(const ST *__restrict__ k, const ST *__restrict__ v, const float *__restrict__ g,
                    const uint8_t *__restrict__ route, const float *__restrict__ u, const int32_t *__restrict__ path,
                    const int32_t *__restrict__ n_path, float *__restrict__ state, ST *__restrict__ k_cache,
                    ST *__restrict__ v_cache, int32_t *__restrict__ cache_len, int cap, int H, int T, float norm_eps,
                    int32_t *status) {
-    constexpr int kVec = D / 4, kGroups = kCommitThreads / kVec, kRows = D / kGroups;
+    constexpr int kVec = D / 4, kGroups = kCommitThreads / kVec, kRows = D / kGroups, V = D / 32;
+    using Piece = typename RowPiece<ST, V>::type;
     extern __shared__ __align__(16) float dyn[];  // [T][D] keys, times what the token counts; [T][D] u
     __shared__ int s_node[kMaxNodes];
     __shared__ float s_alpha[kMaxNodes], s_after[kMaxNodes];
@@ -29,10 +53,13 @@ tree_commit_kernel(const ST *__restrict__ k, const ST *__restrict__ v, const flo
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x, b = bh / H, h = bh - b * H;
     float *sk = dyn, *su = dyn + T * D;
     float4 *S = reinterpret_cast<float4 *>(state + (size_t)bh * D * D) + tid % kVec;
-    const int row0 = tid / kVec;
-    float4 s[kRows];
+    const int row0 = tid / kVec * kRows;
+    float4 s[4];
+    auto load = [&](int q) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) s[r] = S[(size_t)(row0 + r * kGroups) * kVec];
+        for (int r = 0; r < 4; ++r) s[r] = S[(size_t)(row0 + 4 * q + r) * kVec];
+    };
+    load(0);
 
     const int m_raw = n_path[b], m = min(max(m_raw, 0), T), n_raw = cache_len[bh], n_old = min(max(n_raw, 0), cap);
     bool bad = m_raw != m;
@@ -63,56 +90,58 @@ tree_commit_kernel(const ST *__restrict__ k, const ST *__restrict__ v, const flo
         if (n_raw != n_old || (!bad && n_old + kept > cap)) atomicMin(status, (int)NATSL_ERR_CACHE_FULL);
     }
     if (bad || kept > cap - n_old) return;        // (the same for the whole CTA) the pair is left untouched
-    float whole = 1.f;
-    for (int j = 0; j < m; ++j) whole *= s_alpha[j];
+    if (m == 0) return;
     if (tid < m) {
         float x = 1.f;
         for (int j = tid + 1; j < m; ++j) x *= s_alpha[j];
         s_after[tid] = x;
     }
     __syncthreads();
+    const float whole = s_after[0] * s_alpha[0];
     for (int j = warp; j < m; j += kCommitThreads / 32) {
-        const size_t row = (((size_t)b * T + s_node[j]) * H + h) * D + lane * (D / 32);
+        const size_t row = (((size_t)b * T + s_node[j]) * H + h) * D + lane * V;
         const bool fold = s_fold >> j & 1, keep = s_keep >> j & 1;
-        float x[D / 32], ss = 0.f;
+        const Piece kp = *reinterpret_cast<const Piece *>(k + row), vp = *reinterpret_cast<const Piece *>(v + row);
+        float x[V], y[V], ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            x[i] = to_f32(k[row + i]);
-            ss = fmaf(x[i], x[i], ss);
-        }
+        for (int i = 0; i < V; ++i) y[i] = fold ? u[row + i] : 0.f;
+        unpack<V>(kp, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
         float f = s_after[j];
         if (norm_eps >= 0.f) f *= rsqrtf(warp_sum(ss) + norm_eps);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            sk[j * D + lane * (D / 32) + i] = fold ? f * x[i] : 0.f;
-            su[j * D + lane * (D / 32) + i] = fold ? u[row + i] : 0.f;
+        for (int i = 0; i < V; ++i) {
+            sk[j * D + lane * V + i] = fold ? f * x[i] : 0.f;
+            su[j * D + lane * V + i] = y[i];
         }
         if (keep) {
-            const int at = n_old + __popcll(s_keep & ((1ull << j) - 1));
-            ST *kc = k_cache + ((size_t)bh * cap + at) * D + lane * (D / 32), *vc = v_cache + ((size_t)bh * cap + at) * D + lane * (D / 32);
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                kc[i] = k[row + i];
-                vc[i] = v[row + i];
-            }
+            const size_t at = ((size_t)bh * cap + n_old + __popcll(s_keep & ((1ull << j) - 1))) * D + lane * V;
+            *reinterpret_cast<Piece *>(k_cache + at) = kp;
+            *reinterpret_cast<Piece *>(v_cache + at) = vp;
         }
     }
     if (tid == 0 && kept) cache_len[bh] = n_old + kept;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) { s[r].x *= whole; s[r].y *= whole; s[r].z *= whole; s[r].w *= whole; }
-    for (int j = 0; j < m; ++j) {
-        const float4 uu = *reinterpret_cast<const float4 *>(su + j * D + tid % kVec * 4);
+    for (int q = 0; q < kRows / 4; ++q) {
+        float4 o[4];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const float kk = sk[j * D + row0 + r * kGroups];
-            s[r].x = fmaf(kk, uu.x, s[r].x); s[r].y = fmaf(kk, uu.y, s[r].y);
-            s[r].z = fmaf(kk, uu.z, s[r].z); s[r].w = fmaf(kk, uu.w, s[r].w);
+        for (int r = 0; r < 4; ++r) o[r] = make_float4(whole * s[r].x, whole * s[r].y, whole * s[r].z, whole * s[r].w);
+        if (q + 1 < kRows / 4) load(q + 1);
+        for (int j = 0; j < m; ++j) {
+            const float4 uu = *reinterpret_cast<const float4 *>(su + j * D + tid % kVec * 4);
+            const float4 k4 = *reinterpret_cast<const float4 *>(sk + j * D + row0 + 4 * q);
+            const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                o[r].x = fmaf(kk[r], uu.x, o[r].x); o[r].y = fmaf(kk[r], uu.y, o[r].y);
+                o[r].z = fmaf(kk[r], uu.z, o[r].z); o[r].w = fmaf(kk[r], uu.w, o[r].w);
+            }
         }
-    }
-    if (m == 0) return;
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) S[(size_t)(row0 + r * kGroups) * kVec] = s[r];
+        for (int r = 0; r < 4; ++r) S[(size_t)(row0 + 4 * q + r) * kVec] = o[r];
+    }
 }
 
 template <typename ST, int D>

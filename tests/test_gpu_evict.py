@@ -63,6 +63,7 @@ def case(seed, B, H, T, d, lengths, cap, dtype, G=1, norm=False):
     x = make(seed, B, H, T, d, lengths, cap, dtype, unit=not norm)
     rng = np.random.default_rng(seed)
     x["visible"] = rng.integers(-2, cap + 3, (B, T, H)).astype(np.int32)
+    x["visible"][0, 0, 0] = [-2 ** 31, 2 ** 31 - 1][seed % 2]
     x["weight"] = rng.random((B, H, cap)).astype(np.float32)
     x["lse"] = logits(x, scales(d, G, norm)[1], G, norm)
     return x
@@ -162,6 +163,23 @@ def test_eviction_with_ties_and_odd_weights(keep, first, recent):
     w[1, 1] = rng.choice([np.inf, -np.inf, np.nan, 1.0, -1.0, 0.0], 3001)
     w[1, 2] = 1.0 + rng.integers(0, 4, 3001) * 2.0 ** -23           # (they differ in the last bits only)
     evict(k, v, w, np.full((2, 3), 3001, np.int32), keep, first, recent, "f32")
+
+
+@pytest.mark.parametrize("B", [1, 40])
+def test_eviction_of_the_tail(B):
+    """What stays is already in front: nothing moves, the length does."""
+    _, k, v, w = cache(5, B, 4, 500, 64, "bf16")
+    w[:] = np.arange(500, 0, -1)
+    evict(k, v, w, np.full((B, 4), 500, np.int32), 320, 3, 0, "bf16")
+    evict(k, v, w, np.full((B, 4), 500, np.int32), 320, 320, 0, "bf16")
+
+
+@pytest.mark.parametrize("H", [2, 160])
+def test_eviction_of_long_caches(H):
+    """More entries than a CTA holds in registers."""
+    rng, k, v, w = cache(6, 1, H, 9001, 64, "bf16")
+    n = rng.integers(8000, 9002, (1, H)).astype(np.int32)
+    evict(k, v, w, n, 6007, 5, 111, "bf16")
 
 
 def test_eviction_of_stored_lengths_out_of_range():
