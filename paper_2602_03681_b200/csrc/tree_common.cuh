@@ -50,33 +50,40 @@ template <int kHeads, int kRows> struct Sums {
 template <int kHeads, int kRows> struct Nodes {
     unsigned long long above[kRows];              // strict ancestors
     unsigned long long fold, keep;                // nodes that update the state; nodes whose K/V count as retained
-    double total[kRows];                          // sum of g from the context up to and with the node, -inf left out ...
-    int wipes[kRows];                             // ... and counted here
+    float2 total[kRows];                          // sum of g from the context up to and with the node, as two fp32 terms, -inf
+    int wipes[kRows];                             // left out and counted here
     float whole[kRows], beta[kRows], g[kRows];    // whole: exp of that sum
     float rq_la[kRows], rk_la[kRows];             // L2 factors; RMS factors per softmax head
     float rq_sm[kHeads][kRows], rk_sm[kHeads][kRows];
     int parent[kRows];
 };
 
-// Reads the tree of (b, h) and walks every node's path (a parent is always a lower index, so a walk ends).  tid: of kRows
-// threads or more, whose barrier `sync` is.
+// What is read of a node (lane-wise, ahead of the number of nodes: rows behind the last node exist, and are not looked at).
+struct NodeRow { int parent, route; float beta, g; };
+__device__ __forceinline__ NodeRow load_node(const Args &a, int b, int h, int t) {
+    NodeRow x{-1, 0, 0.f, 0.f};
+    if (t < a.T) {
+        const size_t at = ((size_t)b * a.T + t) * a.H + h;
+        x = NodeRow{a.parent[(size_t)b * a.T + t], a.route[at], a.beta[at], a.g[at]};
+    }
+    return x;
+}
+// Walks every node's path (a parent is always a lower index, so a walk ends).  tid: of 64 threads or more, whose barrier `sync`
+// is; row: load_node's of node tid.  Another barrier is due before the result is read.
 template <int kHeads, int kRows, typename Sync>
-__device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, int tid, Nodes<kHeads, kRows> *nd, Sync sync) {
+__device__ __forceinline__ void walk_nodes(const Args &a, int b, int h, int n, int tid, const NodeRow &row, Nodes<kHeads, kRows> *nd, Sync sync) {
     if (tid < 64) {                               // (two whole warps, for the ballots)
-        int par = -1, rv = 0;
-        if (tid < n) {
-            const size_t at = ((size_t)b * a.T + tid) * a.H + h;
-            par = a.parent[(size_t)b * a.T + tid];
-            rv = a.route[at];
-            nd->beta[tid] = a.beta[at];
-            nd->g[tid] = a.g[at];
-            if (par < -1 || par >= tid) {         // not a tree: reported, and taken as a child of the context
-                par = -1;
-                atomicMin(a.status, (int)NATSL_ERR_TREE);
-            }
+        int par = tid < n ? row.parent : -1;
+        if (par < -1 || par >= tid) {             // not a tree: reported, and taken as a child of the context
+            if (tid < n) atomicMin(a.status, (int)NATSL_ERR_TREE);
+            par = -1;
         }
-        if (tid < kRows) nd->parent[tid] = par;
-        const unsigned f = __ballot_sync(0xffffffffu, tid < n && rv != 1), k = __ballot_sync(0xffffffffu, tid < n && rv != 0);
+        if (tid < kRows) {
+            nd->parent[tid] = par;
+            nd->beta[tid] = tid < n ? row.beta : 0.f;
+            nd->g[tid] = row.g;
+        }
+        const unsigned f = __ballot_sync(0xffffffffu, tid < n && row.route != 1), k = __ballot_sync(0xffffffffu, tid < n && row.route != 0);
         if ((tid & 31) == 0) {
             reinterpret_cast<unsigned *>(&nd->fold)[tid >> 5] = f;
             reinterpret_cast<unsigned *>(&nd->keep)[tid >> 5] = k;
@@ -90,33 +97,26 @@ __device__ __forceinline__ void read_nodes(const Args &a, int b, int h, int n, i
     sync();
     if (tid < kRows) {
         unsigned long long up = 0;
-        double sum = 0.0;
+        double sum = 0.0;                         // (in 64 bits: nothing of a short stretch far from the context is lost)
         int wipes = 0;
-        if (tid < n) {
-            auto add = [&](int x) {
-                const float g = nd->g[x];
-                if (g == -INFINITY) ++wipes;
-                else sum += g;
-            };
-            add(tid);
-            for (int x = nd->parent[tid]; x >= 0; x = nd->parent[x]) {
-                up |= 1ull << x;
-                add(x);
-            }
-        } else {
-            nd->beta[tid] = 0.f;
+        for (int x = tid < n ? tid : -1; x >= 0;) {
+            const float g = nd->g[x];
+            wipes += g == -INFINITY;
+            sum += g == -INFINITY ? 0.f : g;
+            x = nd->parent[x];
+            up |= x >= 0 ? 1ull << x : 0ull;
         }
+        const float hi = (float)sum;
         nd->above[tid] = up;
-        nd->total[tid] = sum;
+        nd->total[tid] = make_float2(hi, (float)(sum - (double)hi));
         nd->wipes[tid] = wipes;
-        nd->whole[tid] = wipes || tid >= n ? 0.f : expf((float)sum);
+        nd->whole[tid] = wipes || tid >= n ? 0.f : expf(hi);
     }
 }
-// Decay on the path from its node j (exclusive) to i: the sums' difference in 64 bits, where nothing of a short stretch far from
-// the context is lost, and zero as soon as a g of -inf lies on it.
-template <int kHeads, int kRows>
-__device__ __forceinline__ float decay_of(const Nodes<kHeads, kRows> *nd, int i, int j) {
-    return nd->wipes[i] != nd->wipes[j] ? 0.f : expf((float)(nd->total[i] - nd->total[j]));
+// Decay on the path from its node j (exclusive) to i, and zero as soon as a g of -inf lies on it.
+__device__ __forceinline__ float decay_between(float2 total_i, int wipes_i, float2 total_j, int wipes_j) {
+    const float x = expf((total_i.x - total_j.x) + (total_i.y - total_j.y));
+    return wipes_i != wipes_j ? 0.f : x;
 }
 
 // Nodes of a sequence's tree; a count outside [0, T] counts as the nearer of both and is reported.
@@ -223,19 +223,22 @@ __device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, in
 }
 
 // One cluster per pair.
-template <typename K> cudaError_t launch_clusters(K kernel, const Args &a, int BH, int threads, size_t smem, cudaStream_t st) {
+template <typename K, typename... More>
+cudaError_t launch_clusters(K kernel, const Args &a, int BH, int threads, size_t smem, cudaStream_t st, More... more) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(BH * a.cluster);
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = a.cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (placed while the work before it finishes)
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    cfg.numAttrs = 2;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, more...);
     count_launch();
     return e;
 }

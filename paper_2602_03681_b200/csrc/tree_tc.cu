@@ -347,7 +347,7 @@ __device__ __forceinline__ bool finite_bf16x2(uint32_t x) { return (x & 0x7f80u)
 // odd: a value of those is not finite.
 template <int D, int G, bool kNorm, int R>
 __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t *sm, typename Layout<D, R>::N *nd, int b, int h, int n,
-                          int rank, bool odd) {
+                          int rank, bool odd, const NodeRow &node) {
     using L = Layout<D, R>;
     constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16, kPieces = L::kRowBytes / 16;
     const int tid = threadIdx.x - kHalf, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
@@ -367,11 +367,10 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[k][i] = __ldg(S + (size_t)(16 * k + 2 * c4 + (i & 1) + (i >> 1) * 8) * D + tile * 8);
     };
-    const int tiles = cols / 8;
+    const int tiles = cols / 8, tile0 = 3 - warp;            // (the first warps have the tables)
     float s[kKs][4];
-    if (warp < tiles) load(warp, s);
-    read_nodes(a, b, h, n, tid, nd, sync);
-    if (tid < 2 * kRows) {                        // a row's norms, thread = row of q or k
+    if (tile0 < tiles) load(tile0, s);
+    if (kNorm && tid < 2 * kRows) {               // a row's norms, thread = row of q or k
         const int t = tid % kRows;
         const bool is_k = tid >= kRows;
         const uint8_t *row = sm + (is_k ? L::oK : L::oQ) + t * L::kPitch;
@@ -379,18 +378,21 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float ss = 0.f;
-            if (kNorm)
-                for (int c = g * kPieces / G; c < (g + 1) * kPieces / G; ++c) {
-                    const uint4 y = *reinterpret_cast<const uint4 *>(row + c * 16);
-                    const float2 y0 = bf2(y.x), y1 = bf2(y.y), y2 = bf2(y.z), y3 = bf2(y.w);
-                    ss += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
-                }
-            (is_k ? nd->rk_sm : nd->rq_sm)[g][t] = kNorm ? rsqrtf(ss / ds + a.norm_eps) : 1.f;
+#pragma unroll
+            for (int c = g * kPieces / G; c < (g + 1) * kPieces / G; ++c) {
+                const uint4 y = *reinterpret_cast<const uint4 *>(row + c * 16);
+                const float2 y0 = bf2(y.x), y1 = bf2(y.y), y2 = bf2(y.z), y3 = bf2(y.w);
+                ss += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
+            }
+            (is_k ? nd->rk_sm : nd->rq_sm)[g][t] = rsqrtf(ss / ds + a.norm_eps);
             all += ss;
         }
-        (is_k ? nd->rk_la : nd->rq_la)[t] = kNorm ? rsqrtf(all + a.norm_eps) : 1.f;
+        (is_k ? nd->rk_la : nd->rq_la)[t] = rsqrtf(all + a.norm_eps);
     }
+    walk_nodes(a, b, h, n, tid, node, nd, sync);
     sync();
+    auto rq_la = [&](int t) { return kNorm ? nd->rq_la[t] : 1.f; };
+    auto rk_la = [&](int t) { return kNorm ? nd->rk_la[t] : 1.f; };
     const uint32_t q_at = tc::smem_u32(sm + L::oQ), k_at = tc::smem_u32(sm + L::oK), v_at = tc::smem_u32(sm + L::oV);
 
     // ---- the tables: a warp has 16 rows, all columns.  What u takes from u goes to shared memory, what the read-out takes
@@ -425,45 +427,71 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                 mma_bf16(qk[k * 16 / ds][i], aq[1], bf[2], bf[3]);
             }
         }
+        // bit 8 i + x of a row's words: column 8 i + 2 c4 + x
+        const int t0 = warp * 16 + g4, sh = G > 1 ? sc : 0;
+        unsigned fold[2][2], seen[2][2];
+        float bt[2], fq[2], f[2], m[2] = {-INFINITY, -INFINITY}, z[2] = {0.f, 0.f};
+        float2 total[2];
+        int wipes[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int t = warp * 16 + r * 8 + g4;
-            const unsigned long long path = t < n ? nd->above[t] | 1ull << t : 0ull, seen = path & nd->keep, fold = path & nd->fold;
-            const float bt = nd->beta[t] * nd->rk_la[t], fq = a.scale_la * nd->rq_la[t];
-            const float f = a.scale_sm * kLog2e * nd->rq_sm[G > 1 ? sc : 0][t];
-            float m = -INFINITY, z = 0.f, y[kNt][2];
+            const int t = t0 + 8 * r;
+            const unsigned long long path = t < n ? nd->above[t] | 1ull << t : 0ull;
+            const unsigned long long pf = (path & nd->fold) >> (2 * c4), ps = (path & nd->keep) >> (2 * c4);
+            fold[r][0] = (unsigned)pf; fold[r][1] = (unsigned)(pf >> 32);
+            seen[r][0] = (unsigned)ps; seen[r][1] = (unsigned)(ps >> 32);
+            bt[r] = nd->beta[t] * rk_la(t);
+            fq[r] = a.scale_la * rq_la(t);
+            f[r] = a.scale_sm * kLog2e * (kNorm ? nd->rq_sm[sh][t] : 1.f);
+            total[r] = nd->total[t];
+            wipes[r] = nd->wipes[t];
+        }
 #pragma unroll
-            for (int i = 0; i < kNt; ++i) {
-                float w[2];
+        for (int i = 0; i < kNt; ++i) {
+            float w[2][2];
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int j = i * 8 + 2 * c4 + x;
-                    float q = qk[0][i][2 * r + x];
-                    y[i][x] = G > 1 && sc ? qk[G - 1][i][2 * r + x] : q;
-                    if (G > 1) q += qk[G - 1][i][2 * r + x];
-                    const float decay = fold >> j & 1 ? decay_of(nd, t, j) * nd->rk_la[j] : 0.f;
-                    w[x] = fold >> j & 1 ? fq * decay * q : 0.f;
-                    if (j < t) tab[j * kRows + t] = fold >> j & 1 ? bt * decay * kk[i][2 * r + x] : 0.f;
-                    y[i][x] = seen >> j & 1 ? y[i][x] * f * nd->rk_sm[G > 1 ? sc : 0][j] : -INFINITY;
-                    m = fmaxf(m, y[i][x]);
+            for (int x = 0; x < 2; ++x) {
+                const int j = i * 8 + 2 * c4 + x;
+                const float2 total_j = nd->total[j];
+                const int wipes_j = nd->wipes[j];
+                const float rk = rk_la(j), rs = kNorm ? nd->rk_sm[sh][j] : 1.f;
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const bool folds = fold[r][i / 4] >> (8 * (i & 3) + x) & 1u, sees = seen[r][i / 4] >> (8 * (i & 3) + x) & 1u;
+                    float q = qk[0][i][2 * r + x], &y = qk[0][i][2 * r + x];
+                    if (G > 1) {
+                        y = sc ? qk[G - 1][i][2 * r + x] : y;
+                        q += qk[G - 1][i][2 * r + x];
+                    }
+                    const float decay = decay_between(total[r], wipes[r], total_j, wipes_j) * rk;
+                    w[r][x] = folds ? fq[r] * decay * q : 0.f;
+                    if (j < t0 + 8 * r) tab[j * kRows + t0 + 8 * r] = folds ? bt[r] * decay * kk[i][2 * r + x] : 0.f;
+                    y = sees ? y * f[r] * rs : -INFINITY;
+                    m[r] = fmaxf(m[r], y);
                 }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
                 uint32_t w2[2];
-                split2(w[0], w[1], w2);
+                split2(w[r][0], w[r][1], w2);
                 bh_f[i / 2][(i & 1) * 2 + r] = w2[0];
                 bl_f[i / 2][(i & 1) * 2 + r] = w2[1];
             }
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            const float mu = m == -INFINITY ? 0.f : m;
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            m[r] = fmaxf(m[r], __shfl_xor_sync(0xffffffffu, m[r], 1));
+            m[r] = fmaxf(m[r], __shfl_xor_sync(0xffffffffu, m[r], 2));
+            const float mu = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
             for (int i = 0; i < kNt; ++i) {
-                const float p0 = tc::ex2_ftz(y[i][0] - mu), p1 = tc::ex2_ftz(y[i][1] - mu);
-                z += p0 + p1;
+                const float p0 = tc::ex2_ftz(qk[0][i][2 * r] - mu), p1 = tc::ex2_ftz(qk[0][i][2 * r + 1] - mu);
+                z[r] += p0 + p1;
                 p_f[i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
             }
-            z += __shfl_xor_sync(0xffffffffu, z, 1);
-            z += __shfl_xor_sync(0xffffffffu, z, 2);
-            if (c4 == 0) { sums->tree_m[sc][t] = m; sums->tree_z[sc][t] = z; }
+            z[r] += __shfl_xor_sync(0xffffffffu, z[r], 1);
+            z[r] += __shfl_xor_sync(0xffffffffu, z[r], 2);
+            if (c4 == 0) { sums->tree_m[sc][t0 + 8 * r] = m[r]; sums->tree_z[sc][t0 + 8 * r] = z[r]; }
         }
     }
 
@@ -472,7 +500,7 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
     float acc[kUnits][2 * R][4];
 #pragma unroll
     for (int un = 0; un < kUnits; ++un) {
-        const int tile = warp + 4 * un;
+        const int tile = tile0 + 4 * un;
         if (tile >= tiles) break;
         if (un) load(tile, s);
 #pragma unroll
@@ -496,7 +524,7 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
     sync();                                       // k has been read: the right-hand sides take its place
 #pragma unroll
     for (int un = 0; un < kUnits; ++un) {
-        const int tile = warp + 4 * un, at = tile * 8 + 2 * c4;
+        const int tile = tile0 + 4 * un, at = tile * 8 + 2 * c4;
         if (tile >= tiles) break;
 #pragma unroll
         for (int m = 0; m < 2 * R; ++m)
@@ -505,63 +533,65 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                 const int t = (m % R) * 16 + r * 8 + g4;
                 const float x0 = acc[un][m][2 * r], x1 = acc[un][m][2 * r + 1];
                 if (m < R) {
-                    const float fk = nd->whole[t] * nd->rk_la[t], bt = nd->beta[t];
+                    const float fk = nd->whole[t] * rk_la(t), bt = nd->beta[t];
                     const float2 v = bf2(*reinterpret_cast<const uint32_t *>(sm + L::oV + t * L::kPitchV + at * 2));
                     *reinterpret_cast<float2 *>(su + t * cols + at) =
                         t < n ? make_float2(bt * (v.x - fk * x0), bt * (v.y - fk * x1)) : make_float2(0.f, 0.f);
                 } else {
-                    const float fq = a.scale_la * nd->whole[t] * nd->rq_la[t];
+                    const float fq = a.scale_la * nd->whole[t] * rq_la(t);
                     *reinterpret_cast<float2 *>(so + t * cols + at) = make_float2(fq * x0, fq * x1);
                 }
             }
     }
     sync();
-    // ---- the substitution: a thread's column, by blocks of 16 nodes.  A node that u_j does not reach has a zero in the table;
-    // where u_j is not finite, the paths are asked. ----
+    // ---- the substitution: a thread's column, by blocks of 16 nodes.  A node that u_j does not reach has a zero in the table; a
+    // block in which something is not finite is done again, along the paths. ----
     if (tid < cols) {
         const unsigned long long fold = nd->fold;
         float *col = su + tid;
         for (int t0 = 0; t0 < n; t0 += 16) {
-            float r[16];
+            const unsigned folds = (unsigned)(fold >> t0);
+            float r[16], sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) r[i] = col[(t0 + i) * cols];
 #pragma unroll 4
             for (int j = 0; j < t0; ++j) {
                 const float u = col[j * cols], *row = tab + j * kRows + t0;
-                if (finite(u)) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const float4 w = *reinterpret_cast<const float4 *>(row + i);
-                        r[i] = fmaf(-w.x, u, r[i]); r[i + 1] = fmaf(-w.y, u, r[i + 1]);
-                        r[i + 2] = fmaf(-w.z, u, r[i + 2]); r[i + 3] = fmaf(-w.w, u, r[i + 3]);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (nd->above[t0 + i] >> j & 1) r[i] = fmaf(-row[i], u, r[i]);
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 w = *reinterpret_cast<const float4 *>(row + i);
+                    r[i] = fmaf(-w.x, u, r[i]); r[i + 1] = fmaf(-w.y, u, r[i + 1]);
+                    r[i + 2] = fmaf(-w.z, u, r[i + 2]); r[i + 3] = fmaf(-w.w, u, r[i + 3]);
                 }
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
-                const float u = r[j] = fold >> (t0 + j) & 1 ? r[j] : 0.f, *row = tab + (t0 + j) * kRows + t0;
-                if (finite(u)) {
+                const float *row = tab + (t0 + j) * kRows + t0;
+                r[j] = folds >> j & 1u ? r[j] : 0.f;
+                sum = fmaf(r[j], 0.f, sum);       // (NaN from what is not finite)
 #pragma unroll
-                    for (int i = (j + 1) / 4 * 4; i < 16; i += 4) {
-                        const float4 w = *reinterpret_cast<const float4 *>(row + i);
-                        if (i > j) r[i] = fmaf(-w.x, u, r[i]);
-                        if (i + 1 > j) r[i + 1] = fmaf(-w.y, u, r[i + 1]);
-                        if (i + 2 > j) r[i + 2] = fmaf(-w.z, u, r[i + 2]);
-                        if (i + 3 > j) r[i + 3] = fmaf(-w.w, u, r[i + 3]);
-                    }
-                } else {
-                    odd = true;
-#pragma unroll
-                    for (int i = j + 1; i < 16; ++i)
-                        if (nd->above[t0 + i] >> (t0 + j) & 1) r[i] = fmaf(-row[i], u, r[i]);
+                for (int i = (j + 1) / 4 * 4; i < 16; i += 4) {
+                    const float4 w = *reinterpret_cast<const float4 *>(row + i);
+                    if (i > j) r[i] = fmaf(-w.x, r[j], r[i]);
+                    if (i + 1 > j) r[i + 1] = fmaf(-w.y, r[j], r[i + 1]);
+                    if (i + 2 > j) r[i + 2] = fmaf(-w.z, r[j], r[i + 2]);
+                    if (i + 3 > j) r[i + 3] = fmaf(-w.w, r[j], r[i + 3]);
                 }
             }
+            if (sum == 0.f) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) col[(t0 + i) * cols] = r[i];
+                for (int i = 0; i < 16; ++i) col[(t0 + i) * cols] = r[i];
+            } else {
+                odd = true;
+                for (int t = t0; t < min(n, t0 + 16); ++t) {
+                    float x = col[t * cols];
+                    for (unsigned long long w = nd->above[t] & fold; w; w &= w - 1) {
+                        const int j = __ffsll(w) - 1;
+                        x = fmaf(-tab[j * kRows + t], col[j * cols], x);
+                    }
+                    col[t * cols] = fold >> t & 1 ? x : 0.f;
+                }
+            }
         }
     }
     if (odd) s_odd = 1;
@@ -668,6 +698,9 @@ __global__ void __launch_bounds__(kThreads, Layout<D, R>::kCtas) tree_tc_kernel(
     extern __shared__ __align__(128) uint8_t dyn_tc[];
     __shared__ typename L::N nodes;
     const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, tid = threadIdx.x;
+    tc::grid_dependency_wait();
+    tc::launch_dependents();
+    const NodeRow node = load_node(a, b, h, tid >= kHalf ? tid - kHalf : a.T);
     const int n = nodes_of(a, b), cols = D / a.cluster;
     const Stream<D, R> in(a, dyn_tc, bh, tid, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
     typename L::S *sums = reinterpret_cast<typename L::S *>(dyn_tc);
@@ -702,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, R>::kCtas) tree_tc_kernel(
     }
     odd = __syncthreads_or(odd);
     if (tid < kHalf) cache_part<D, G, kNorm, R>(a, sums, dyn_tc, in, n);
-    else tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank, odd);
+    else tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank, odd, node);
     join_rows<__nv_bfloat16, D>(a, b, h, n, rank, sums, reinterpret_cast<const float *>(dyn_tc + L::oRing), L::kAccPitch,
                                 reinterpret_cast<const float *>(dyn_tc + L::oO), reinterpret_cast<const float *>(dyn_tc + L::oT));
 }
