@@ -126,9 +126,8 @@ __device__ __forceinline__ int nodes_of(const Args &a, int b) {
 }
 
 // The cluster's barrier: what its threads have written to shared memory is there for all of them.
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // `p`'s counterpart in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t remote(const void *p, int rank) {
     uint32_t r;
@@ -160,7 +159,9 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
     float2 w = make_float2(0.5f, 0.5f), w_next = w;
     auto weights = [&](int t) { return *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t) * a.H + h) * 2); };
     if (a.w && t < n) w_next = weights(t);
-    cluster_sync();
+    cluster_arrive();
+    cluster_wait();
+    bool read = false;
     for (; t < n; t += step) {
         w = w_next;
         if (a.w && t + step < n) w_next = weights(t + step);
@@ -209,10 +210,15 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
             out[0] = from_f32<ST>(y[0]);
             out[1] = from_f32<ST>(y[1]);
         }
+        if (t + step >= n) {                      // (the warp's last row has arrived)
+            cluster_arrive();
+            read = true;
+        }
         if (a.lse && lane % ls == 0)
             a.lse[(((size_t)b * a.H + h) * G + sg) * a.T + t] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * kLn2;
     }
-    cluster_sync();                               // nobody's shared memory goes while a neighbour still reads it
+    if (!read) cluster_arrive();
+    cluster_wait();                               // nobody's shared memory goes while a neighbour still reads it
 }
 template <typename ST, int D, typename S>
 __device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, int rank, const S *sums, const float *acc, int acc_pitch,

@@ -2,13 +2,13 @@
 // tree_simt.cu's; here the products are warp-level MMAs: a tree has 1 to 64 query rows, far below a tcgen05 tile of 128, and
 // the call is bound by reading the retained K/V once.
 //
-// A CTA has two halves that work side by side and meet at the end.  Four warps read the CTA's share of the cache: tiles of 64
+// A CTA has two halves that work side by side and meet at the end.  Half of the warps read the CTA's share of the cache: tiles of 64
 // keys through a ring of asynchronous copies, K and V in turns.  They share the tile by keys (and, beyond 16 nodes, by two
-// halves of the rows), each with its own running maximum and sum, so that a key's row leaves shared memory once (twice)
+// groups of 16), each with its own running maximum and sum, so that a key's row leaves shared memory once (twice)
 // whatever the number of nodes; the warps' results meet at the end.  A running maximum moves only when a logit exceeds it by
 // 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's own precision); their sum is taken before the rounding.
 //
-// The other four warps compute the tree's own part, for the CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32 state as three bf16 terms that
+// The other warps compute the tree's own part, for the CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32 state as three bf16 terms that
 // together hold all of its 24 bits, so that u, which goes into the state at the commit, is as exact as on CUDA cores; the
 // substitution for u in fp32, a thread per column, by blocks of 16 nodes without a look at the tree's shape (the table is
 // zero off the path); the read-outs as MMAs again, u and the table as two bf16 terms each (2^-16).  Zeros in the place of
@@ -22,7 +22,7 @@ namespace {
 
 using namespace tree;
 
-constexpr int kThreads = 256, kHalf = 128, kTileKeys = 64;
+constexpr int kTileKeys = 64;
 using tc::ldmatrix_x4;
 using tc::ldmatrix_x4_trans;
 
@@ -49,9 +49,10 @@ template <int D, int R> struct Layout {
     static constexpr int kRows = 16 * R;                     // nodes, padded
     using S = Sums<2, kRows>;
     using N = Nodes<2, kRows>;
-    static constexpr int kCtas = R == 4 ? 1 : 2;             // per multiprocessor
-    static constexpr int kMt = R == 4 ? 2 : 1;               // cache: row tiles per warp
-    static constexpr int kRowGroups = R / kMt, kKeyGroups = 4 / kRowGroups, kWarpKeys = kTileKeys / kKeyGroups;
+    // 16 warps per multiprocessor: two CTAs of 8, or one of 16.  Half of a CTA's warps read the cache, each 16 rows and a share of
+    // the tile's keys.
+    static constexpr int kCtas = R == 4 ? 1 : 2, kWarps = R == 4 ? 8 : 4, kHalf = 32 * kWarps, kThreads = 2 * kHalf;
+    static constexpr int kKeyGroups = kWarps / R, kWarpKeys = kTileKeys / kKeyGroups;
     static constexpr int kRowBytes = D * 2, kTileBytes = kTileKeys * kRowBytes;
     static constexpr int kSlots = R == 4 ? (D == 128 ? 7 : 8) : D == 128 ? 4 : 6;
     static constexpr int kAccPitch = D + 4;
@@ -59,9 +60,11 @@ template <int D, int R> struct Layout {
     static constexpr int kPitch = kRowBytes + 16;            // (an odd number of 16-byte pieces: eight rows, eight banks)
     static constexpr int kPitchV = kCols * 2 + 16;
     static constexpr int oQ = sizeof(S), oK = oQ + kRows * kPitch, oV = oK + kRows * kPitch, oTab = oV + kRows * kPitchV;
-    static constexpr int oO = oTab + kRows * kRows * 4, oT = oO + kRows * kCols * 4;      // the read-outs: linear, over the tree
+    // u and the linear read-out of the CTA's columns (the sums over the tree's V: over k); the probabilities over the tree, bf16
+    static constexpr int oU = oTab + kRows * kRows * 4, oO = oU + kRows * kCols * 4, oP = oO + kRows * kCols * 4;
+    static constexpr int kPitchP = kRows * 2 + 16;
     // the ring (16-byte pieces swizzled by row); at the end the key groups' results, the first one's place the CTA's
-    static constexpr int oRing = (oT + kRows * kCols * 4 + 127) / 128 * 128, kRing = kSlots * kTileBytes;
+    static constexpr int oRing = (oP + kRows * kPitchP + 127) / 128 * 128, kRing = kSlots * kTileBytes;
     static constexpr int kMerge = kKeyGroups * kRows * kAccPitch * 4;
     static_assert(kMerge <= kRing, "the key groups' results lie in the ring");
     static constexpr int kTotal = oRing + kRing;
@@ -70,12 +73,12 @@ template <int D, int R> struct Layout {
 // The CTA's share of the cache: units 0, 1, 2, ... are K of tile 0, V of tile 0, K of tile 1, ...
 template <int D, int R> struct Stream {
     using L = Layout<D, R>;
-    static constexpr int kPieces = L::kRowBytes / 16, kStep = kHalf / kPieces;
+    static constexpr int kPieces = L::kRowBytes / 16, kStep = L::kHalf / kPieces;
     const uint8_t *kc, *vc;
     uint32_t ring, dst0;
     int row0, from, to, units;
     __device__ Stream(const Args &a, uint8_t *sm, int bh, int tid, const Share &c) {
-        const int piece = tid % kPieces;          // thread = 16-byte piece of every eighth (sixteenth) row of a tile
+        const int piece = tid % kPieces;          // thread = 16-byte piece of every kStep-th row of a tile
         row0 = tid / kPieces;
         kc = reinterpret_cast<const uint8_t *>(a.k_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
         vc = reinterpret_cast<const uint8_t *>(a.v_cache) + (size_t)bh * a.cap * L::kRowBytes + piece * 16;
@@ -104,54 +107,48 @@ template <int D, int R> struct Stream {
 template <int D, int G, bool kNorm, int R>
 __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t *sm, const Stream<D, R> &in, int n_nodes) {
     using L = Layout<D, R>;
-    constexpr int ds = D / G, kMt = L::kMt, kNt = L::kWarpKeys / 8, kKs = ds / 16;
+    constexpr int ds = D / G, kNt = L::kWarpKeys / 8, kKs = ds / 16, kHalf = L::kHalf;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
-    const int rg = warp / L::kKeyGroups, kg = warp - rg * L::kKeyGroups, r0 = rg * 16 * kMt;
+    const int rg = warp / L::kKeyGroups, kg = warp - rg * L::kKeyGroups, r0 = rg * 16;
     const uint32_t q_at = tc::smem_u32(sm + L::oQ) + (r0 + (lane & 15)) * L::kPitch + (lane >> 4) * 16;
-    auto load_q = [&](int m, int k, uint32_t (&x)[4]) { ldmatrix_x4(q_at + m * 16 * L::kPitch + k * 32, x); };
+    auto load_q = [&](int k, uint32_t (&x)[4]) { ldmatrix_x4(q_at + k * 32, x); };
 
     // each row's factor to base-2 logits
-    float f[kMt][2][kNorm ? G : 1];
+    float f[2][kNorm ? G : 1];
+    f[0][0] = f[1][0] = a.scale_sm * kLog2e;
+    if (kNorm) {
 #pragma unroll
-    for (int m = 0; m < kMt; ++m) {
-        f[m][0][0] = f[m][1][0] = a.scale_sm * kLog2e;
-        if (kNorm) {
+        for (int s = 0; s < G; ++s) {
+            float ss[2] = {0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < G; ++s) {
-                float ss[2] = {0.f, 0.f};
+            for (int k = s * kKs; k < (s + 1) * kKs; ++k) {
+                uint32_t x[4];
+                load_q(k, x);
 #pragma unroll
-                for (int k = s * kKs; k < (s + 1) * kKs; ++k) {
-                    uint32_t x[4];
-                    load_q(m, k, x);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 y = bf2(x[i]);
-                        ss[i & 1] = fmaf(y.x, y.x, fmaf(y.y, y.y, ss[i & 1]));
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const float2 y = bf2(x[i]);
+                    ss[i & 1] = fmaf(y.x, y.x, fmaf(y.y, y.y, ss[i & 1]));
                 }
+            }
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    ss[r] += __shfl_xor_sync(0xffffffffu, ss[r], 1);
-                    ss[r] += __shfl_xor_sync(0xffffffffu, ss[r], 2);
-                    f[m][r][s] = a.scale_sm * kLog2e * rsqrtf(ss[r] / ds + a.norm_eps);
-                }
+            for (int r = 0; r < 2; ++r) {
+                ss[r] += __shfl_xor_sync(0xffffffffu, ss[r], 1);
+                ss[r] += __shfl_xor_sync(0xffffffffu, ss[r], 2);
+                f[r][s] = a.scale_sm * kLog2e * rsqrtf(ss[r] / ds + a.norm_eps);
             }
         }
     }
-    float o[kMt][D / 8][4], mx[G][kMt][2], z[G][kMt][2];
+    float o[D / 8][4], mx[G][2], z[G][2];
 #pragma unroll
-    for (int m = 0; m < kMt; ++m) {
+    for (int i = 0; i < D / 8; ++i)
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
+        for (int x = 0; x < 4; ++x) o[i][x] = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) o[m][i][x] = 0.f;
+    for (int s = 0; s < G; ++s)
 #pragma unroll
-        for (int s = 0; s < G; ++s)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) { mx[s][m][r] = -INFINITY; z[s][m][r] = 0.f; }
-    }
+        for (int r = 0; r < 2; ++r) { mx[s][r] = -INFINITY; z[s][r] = 0.f; }
     const int key0 = kg * L::kWarpKeys;
-    uint32_t pf[G][kMt][kNt / 2][4];
+    uint32_t pf[G][kNt / 2][4];
     auto turn = [&](int u) {                      // unit u is there, and every warp is done with unit u - 1 ...
         cp_async_wait<L::kSlots - 2>();
         tc::named_barrier_sync(1, kHalf);
@@ -164,30 +161,24 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
             const uint32_t kt = in.slot(u);
 #pragma unroll
             for (int s = 0; s < G; ++s) {
-                float x[kMt][kNt][4], kk[kNt];
+                float x[kNt][4], kk[kNt];
 #pragma unroll
                 for (int i = 0; i < kNt; ++i) {
                     kk[i] = 0.f;
 #pragma unroll
-                    for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) x[m][i][y] = 0.f;
+                    for (int y = 0; y < 4; ++y) x[i][y] = 0.f;
                 }
 #pragma unroll
                 for (int k = s * kKs; k < (s + 1) * kKs; ++k) {
-                    uint32_t qf[kMt][4];
-#pragma unroll
-                    for (int m = 0; m < kMt; ++m) load_q(m, k, qf[m]);
+                    uint32_t qf[4];
+                    load_q(k, qf);
 #pragma unroll
                     for (int i = 0; i < kNt; i += 2) {
                         const int row = key0 + i * 8 + (lane & 7) + (lane >> 4) * 8;
                         uint32_t bf[4];
                         ldmatrix_x4(kt + row * L::kRowBytes + (((2 * k + ((lane >> 3) & 1)) ^ (row & 7)) << 4), bf);
-#pragma unroll
-                        for (int m = 0; m < kMt; ++m) {
-                            mma_bf16(x[m][i], qf[m], bf[0], bf[1]);
-                            mma_bf16(x[m][i + 1], qf[m], bf[2], bf[3]);
-                        }
+                        mma_bf16(x[i], qf, bf[0], bf[1]);
+                        mma_bf16(x[i + 1], qf, bf[2], bf[3]);
                         if (kNorm) {              // the key's sum of squares rides along
 #pragma unroll
                             for (int y = 0; y < 4; ++y) {
@@ -208,57 +199,55 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
                         w0 = __shfl_sync(0xffffffffu, w, c4 * 8);
                         w1 = __shfl_sync(0xffffffffu, w, c4 * 8 + 4);
                     }
-                    const bool in0 = i * 8 + 2 * c4 < left, in1 = i * 8 + 2 * c4 + 1 < left;
 #pragma unroll
-                    for (int m = 0; m < kMt; ++m)
+                    for (int r = 0; r < 2; ++r) {
+                        const float fr = f[r][kNorm ? s : 0];
+                        x[i][2 * r] *= fr * w0;
+                        x[i][2 * r + 1] *= fr * w1;
+                    }
+                }
+                if (left < L::kWarpKeys) {
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const float fr = f[m][r][kNorm ? s : 0];
-                            x[m][i][2 * r] = in0 ? x[m][i][2 * r] * (fr * w0) : -INFINITY;
-                            x[m][i][2 * r + 1] = in1 ? x[m][i][2 * r + 1] * (fr * w1) : -INFINITY;
-                        }
+                    for (int i = 0; i < kNt; ++i)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y)
+                            if (i * 8 + 2 * c4 + (y & 1) >= left) x[i][y] = -INFINITY;
                 }
                 bool raise = false;
-                float top[kMt][2];
+                float top[2];
 #pragma unroll
-                for (int m = 0; m < kMt; ++m)
+                for (int r = 0; r < 2; ++r) {
+                    float y = x[0][2 * r];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float y = x[m][0][2 * r];
-#pragma unroll
-                        for (int i = 0; i < kNt; ++i) y = tc::max3(y, x[m][i][2 * r], x[m][i][2 * r + 1]);
-                        y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
-                        top[m][r] = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
-                        raise |= top[m][r] > mx[s][m][r] + 8.f;
-                    }
+                    for (int i = 0; i < kNt; ++i) y = tc::max3(y, x[i][2 * r], x[i][2 * r + 1]);
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
+                    top[r] = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
+                    raise |= top[r] > mx[s][r] + 8.f;
+                }
                 if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-                    for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const float m1 = fmaxf(mx[s][m][r], top[m][r]);
-                            const float e = mx[s][m][r] == m1 ? 1.f : tc::ex2_ftz(mx[s][m][r] - m1);
-                            mx[s][m][r] = m1;
-                            z[s][m][r] *= e;
-#pragma unroll
-                            for (int i = s * ds / 8; i < (s + 1) * ds / 8; ++i) {
-                                o[m][i][2 * r] *= e;
-                                o[m][i][2 * r + 1] *= e;
-                            }
-                        }
-                }
-#pragma unroll
-                for (int m = 0; m < kMt; ++m)
-#pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float mu = mx[s][m][r] == -INFINITY ? 0.f : mx[s][m][r];
+                        const float m1 = fmaxf(mx[s][r], top[r]);
+                        const float e = mx[s][r] == m1 ? 1.f : tc::ex2_ftz(mx[s][r] - m1);
+                        mx[s][r] = m1;
+                        z[s][r] *= e;
 #pragma unroll
-                        for (int i = 0; i < kNt; ++i) {
-                            const float p0 = tc::ex2_ftz(x[m][i][2 * r] - mu), p1 = tc::ex2_ftz(x[m][i][2 * r + 1] - mu);
-                            z[s][m][r] += p0 + p1;
-                            pf[s][m][i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
+                        for (int i = s * ds / 8; i < (s + 1) * ds / 8; ++i) {
+                            o[i][2 * r] *= e;
+                            o[i][2 * r + 1] *= e;
                         }
                     }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float mu = mx[s][r] == -INFINITY ? 0.f : mx[s][r];
+#pragma unroll
+                    for (int i = 0; i < kNt; ++i) {
+                        const float p0 = tc::ex2_ftz(x[i][2 * r] - mu), p1 = tc::ex2_ftz(x[i][2 * r + 1] - mu);
+                        z[s][r] += p0 + p1;
+                        pf[s][i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
+                    }
+                }
             }
         }
         turn(u + 1);
@@ -271,11 +260,8 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
                 for (int n = 0; n < D / 16; ++n) {
                     uint32_t bf[4];
                     ldmatrix_x4_trans(vt + row * L::kRowBytes + (((2 * n + (lane >> 4)) ^ (row & 7)) << 4), bf);
-#pragma unroll
-                    for (int m = 0; m < kMt; ++m) {
-                        mma_bf16(o[m][2 * n], pf[n * 16 / ds][m][i], bf[0], bf[1]);
-                        mma_bf16(o[m][2 * n + 1], pf[n * 16 / ds][m][i], bf[2], bf[3]);
-                    }
+                    mma_bf16(o[2 * n], pf[n * 16 / ds][i], bf[0], bf[1]);
+                    mma_bf16(o[2 * n + 1], pf[n * 16 / ds][i], bf[2], bf[3]);
                 }
             }
         }
@@ -286,21 +272,19 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
     tc::named_barrier_sync(1, kHalf);
     float *acc = reinterpret_cast<float *>(sm + L::oRing);
 #pragma unroll
-    for (int m = 0; m < kMt; ++m)
+    for (int r = 0; r < 2; ++r) {
+        const int t = r0 + r * 8 + g4;
+        float *to = acc + (kg * L::kRows + t) * L::kAccPitch + 2 * c4;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int t = r0 + m * 16 + r * 8 + g4;
-            float *to = acc + (kg * L::kRows + t) * L::kAccPitch + 2 * c4;
+        for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2 *>(to + 8 * i) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) *reinterpret_cast<float2 *>(to + 8 * i) = make_float2(o[m][i][2 * r], o[m][i][2 * r + 1]);
-#pragma unroll
-            for (int s = 0; s < G; ++s) {
-                float y = z[s][m][r];
-                y += __shfl_xor_sync(0xffffffffu, y, 1);
-                y += __shfl_xor_sync(0xffffffffu, y, 2);
-                if (c4 == 0) { s_m[s][kg][t] = mx[s][m][r]; s_z[s][kg][t] = y; }
-            }
+        for (int s = 0; s < G; ++s) {
+            float y = z[s][r];
+            y += __shfl_xor_sync(0xffffffffu, y, 1);
+            y += __shfl_xor_sync(0xffffffffu, y, 2);
+            if (c4 == 0) { s_m[s][kg][t] = mx[s][r]; s_z[s][kg][t] = y; }
         }
+    }
     tc::named_barrier_sync(1, kHalf);
     for (int i = tid; i < n_nodes * (D / 4); i += kHalf) {
         const int t = i / (D / 4), x = (i - t * (D / 4)) * 4, s = x / ds;
@@ -349,27 +333,30 @@ template <int D, int G, bool kNorm, int R>
 __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t *sm, typename Layout<D, R>::N *nd, int b, int h, int n,
                           int rank, bool odd, const NodeRow &node) {
     using L = Layout<D, R>;
-    constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16, kPieces = L::kRowBytes / 16;
+    constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16, kPieces = L::kRowBytes / 16, kHalf = L::kHalf, kWarps = L::kWarps;
     const int tid = threadIdx.x - kHalf, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
     const int bh = b * a.H + h, cols = D / a.cluster, c0 = rank * cols, sc = c0 / ds;   // sc: the columns' softmax head
     auto sync = [] { tc::named_barrier_sync(2, kHalf); };
     float *tab = reinterpret_cast<float *>(sm + L::oTab);    // [j][i], i > j: what u_i takes from u_j
-    float *su = reinterpret_cast<float *>(sm + L::oK);       // (over k)
-    float *so = reinterpret_cast<float *>(sm + L::oO), *st = reinterpret_cast<float *>(sm + L::oT);
+    float *su = reinterpret_cast<float *>(sm + L::oU), *so = reinterpret_cast<float *>(sm + L::oO);
+    float *st = reinterpret_cast<float *>(sm + L::oK);       // (over k)
 
     // A tile of eight state columns as the B fragments of all products with it: rows 2 c4, + 1, + 8, + 9 of a step of 16.
     __shared__ int s_odd;
     if (tid == 0) s_odd = 0;
     const float *S = a.state + (size_t)bh * D * D + c0 + g4;
-    auto load = [&](int tile, float (&y)[kKs][4]) {
+    auto load = [&](int tile, int k, float (&y)[4]) {
 #pragma unroll
-        for (int k = 0; k < kKs; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[k][i] = __ldg(S + (size_t)(16 * k + 2 * c4 + (i & 1) + (i >> 1) * 8) * D + tile * 8);
+        for (int i = 0; i < 4; ++i) y[i] = __ldg(S + (size_t)(16 * k + 2 * c4 + (i & 1) + (i >> 1) * 8) * D + tile * 8);
     };
-    const int tiles = cols / 8, tile0 = 3 - warp;            // (the first warps have the tables)
+    // (the first warps have the tables; beyond 32 nodes that is all they do meanwhile)
+    constexpr bool kApart = R == 4;
+    constexpr int kStride = kApart ? kWarps - R : kWarps;
+    const int tiles = cols / 8, tile0 = kApart && warp < R ? tiles : kWarps - 1 - warp;
     float s[kKs][4];
-    if (tile0 < tiles) load(tile0, s);
+    if (tile0 < tiles)
+#pragma unroll
+        for (int k = 0; k < kKs; ++k) load(tile0, k, s[k]);
     if (kNorm && tid < 2 * kRows) {               // a row's norms, thread = row of q or k
         const int t = tid % kRows;
         const bool is_k = tid >= kRows;
@@ -395,44 +382,17 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
     auto rk_la = [&](int t) { return kNorm ? nd->rk_la[t] : 1.f; };
     const uint32_t q_at = tc::smem_u32(sm + L::oQ), k_at = tc::smem_u32(sm + L::oK), v_at = tc::smem_u32(sm + L::oV);
 
-    // ---- the tables: a warp has 16 rows, all columns.  What u takes from u goes to shared memory, what the read-out takes
-    // from u (two terms) and the probabilities stay in registers, as the A fragments of the read-out. ----
-    uint32_t bh_f[kNt / 2][4], bl_f[kNt / 2][4], p_f[kNt / 2][4];
-    if (warp < R) {
-        float kk[kNt][4], qk[G][kNt][4];
-#pragma unroll
-        for (int i = 0; i < kNt; ++i)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                kk[i][x] = 0.f;
-#pragma unroll
-                for (int g = 0; g < G; ++g) qk[g][i][x] = 0.f;
-            }
-#pragma unroll
-        for (int k = 0; k < kKs; k += 2) {
-            uint32_t ak[2][4], aq[2][4];
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                const uint32_t off = (warp * 16 + (lane & 15)) * L::kPitch + (2 * (k + y) + (lane >> 4)) * 16;
-                ldmatrix_x4(k_at + off, ak[y]);
-                ldmatrix_x4(q_at + off, aq[y]);
-            }
-#pragma unroll
-            for (int i = 0; i < kNt; ++i) {
-                uint32_t bf[4];
-                ldmatrix_x4(k_at + (i * 8 + (lane & 7)) * L::kPitch + (2 * k + (lane >> 3)) * 16, bf);
-                mma_bf16(kk[i], ak[0], bf[0], bf[1]);
-                mma_bf16(kk[i], ak[1], bf[2], bf[3]);
-                mma_bf16(qk[k * 16 / ds][i], aq[0], bf[0], bf[1]);
-                mma_bf16(qk[k * 16 / ds][i], aq[1], bf[2], bf[3]);
-            }
-        }
+    // ---- the tables: the first R warps have 16 rows each, all columns.  What u takes from u and the probabilities go to shared
+    // memory; what the read-out takes from u (two terms) stays in registers, as the A fragments of the read-out. ----
+    uint32_t bh_f[kNt / 2][4], bl_f[kNt / 2][4];
+    auto tables = [&] {
         // bit 8 i + x of a row's words: column 8 i + 2 c4 + x
         const int t0 = warp * 16 + g4, sh = G > 1 ? sc : 0;
         unsigned fold[2][2], seen[2][2];
         float bt[2], fq[2], f[2], m[2] = {-INFINITY, -INFINITY}, z[2] = {0.f, 0.f};
         float2 total[2];
         int wipes[2];
+        float y[kNt][4];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const int t = t0 + 8 * r;
@@ -446,36 +406,68 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
             total[r] = nd->total[t];
             wipes[r] = nd->wipes[t];
         }
+        constexpr int kPart = kNt < 4 ? kNt : 4;  // (32 columns at a time: registers)
 #pragma unroll
-        for (int i = 0; i < kNt; ++i) {
-            float w[2][2];
+        for (int i0 = 0; i0 < kNt; i0 += kPart) {
+            float kk[kPart][4], qk[G][kPart][4];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int j = i * 8 + 2 * c4 + x;
-                const float2 total_j = nd->total[j];
-                const int wipes_j = nd->wipes[j];
-                const float rk = rk_la(j), rs = kNorm ? nd->rk_sm[sh][j] : 1.f;
+            for (int i = 0; i < kPart; ++i)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const bool folds = fold[r][i / 4] >> (8 * (i & 3) + x) & 1u, sees = seen[r][i / 4] >> (8 * (i & 3) + x) & 1u;
-                    float q = qk[0][i][2 * r + x], &y = qk[0][i][2 * r + x];
-                    if (G > 1) {
-                        y = sc ? qk[G - 1][i][2 * r + x] : y;
-                        q += qk[G - 1][i][2 * r + x];
-                    }
-                    const float decay = decay_between(total[r], wipes[r], total_j, wipes_j) * rk;
-                    w[r][x] = folds ? fq[r] * decay * q : 0.f;
-                    if (j < t0 + 8 * r) tab[j * kRows + t0 + 8 * r] = folds ? bt[r] * decay * kk[i][2 * r + x] : 0.f;
-                    y = sees ? y * f[r] * rs : -INFINITY;
-                    m[r] = fmaxf(m[r], y);
+                for (int x = 0; x < 4; ++x) {
+                    kk[i][x] = 0.f;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) qk[g][i][x] = 0.f;
                 }
+#pragma unroll
+            for (int k = 0; k < kKs; k += 2) {
+                uint32_t ak[2][4], aq[2][4], bf[kPart][4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const uint32_t off = (warp * 16 + (lane & 15)) * L::kPitch + (2 * (k + x) + (lane >> 4)) * 16;
+                    ldmatrix_x4(k_at + off, ak[x]);
+                    ldmatrix_x4(q_at + off, aq[x]);
+                }
+#pragma unroll
+                for (int i = 0; i < kPart; ++i) ldmatrix_x4(k_at + ((i0 + i) * 8 + (lane & 7)) * L::kPitch + (2 * k + (lane >> 3)) * 16, bf[i]);
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int i = 0; i < kPart; ++i) {
+                        mma_bf16(kk[i], ak[x], bf[i][2 * x], bf[i][2 * x + 1]);
+                        mma_bf16(qk[k * 16 / ds][i], aq[x], bf[i][2 * x], bf[i][2 * x + 1]);
+                    }
             }
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                uint32_t w2[2];
-                split2(w[r][0], w[r][1], w2);
-                bh_f[i / 2][(i & 1) * 2 + r] = w2[0];
-                bl_f[i / 2][(i & 1) * 2 + r] = w2[1];
+            for (int i = 0; i < kPart; ++i) {
+                float w[2][2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int j = (i0 + i) * 8 + 2 * c4 + x, bit = 8 * ((i0 + i) & 3) + x;
+                    const float2 total_j = nd->total[j];
+                    const int wipes_j = nd->wipes[j];
+                    const float rk = rk_la(j), rs = kNorm ? nd->rk_sm[sh][j] : 1.f;
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const bool folds = fold[r][i0 / 4] >> bit & 1u, sees = seen[r][i0 / 4] >> bit & 1u;
+                        float q = qk[0][i][2 * r + x], own = q;
+                        if (G > 1) {
+                            own = sc ? qk[G - 1][i][2 * r + x] : q;
+                            q += qk[G - 1][i][2 * r + x];
+                        }
+                        const float decay = decay_between(total[r], wipes[r], total_j, wipes_j) * rk;
+                        w[r][x] = folds ? fq[r] * decay * q : 0.f;
+                        if (j < t0 + 8 * r) tab[j * kRows + t0 + 8 * r] = folds ? bt[r] * decay * kk[i][2 * r + x] : 0.f;
+                        y[i0 + i][2 * r + x] = sees ? own * f[r] * rs : -INFINITY;
+                        m[r] = fmaxf(m[r], y[i0 + i][2 * r + x]);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    uint32_t w2[2];
+                    split2(w[r][0], w[r][1], w2);
+                    bh_f[(i0 + i) / 2][(i & 1) * 2 + r] = w2[0];
+                    bl_f[(i0 + i) / 2][(i & 1) * 2 + r] = w2[1];
+                }
             }
         }
 #pragma unroll
@@ -485,65 +477,59 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
             const float mu = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
             for (int i = 0; i < kNt; ++i) {
-                const float p0 = tc::ex2_ftz(qk[0][i][2 * r] - mu), p1 = tc::ex2_ftz(qk[0][i][2 * r + 1] - mu);
+                const float p0 = tc::ex2_ftz(y[i][2 * r] - mu), p1 = tc::ex2_ftz(y[i][2 * r + 1] - mu);
                 z[r] += p0 + p1;
-                p_f[i / 2][(i & 1) * 2 + r] = tc::pack_bf162(p0, p1);
+                *reinterpret_cast<uint32_t *>(sm + L::oP + (t0 + 8 * r) * L::kPitchP + (i * 8 + 2 * c4) * 2) = tc::pack_bf162(p0, p1);
             }
             z[r] += __shfl_xor_sync(0xffffffffu, z[r], 1);
             z[r] += __shfl_xor_sync(0xffffffffu, z[r], 2);
             if (c4 == 0) { sums->tree_m[sc][t0 + 8 * r] = m[r]; sums->tree_z[sc][t0 + 8 * r] = z[r]; }
         }
-    }
-
-    // ---- k S0 and q S0, a warp's tiles of eight columns for all rows ----
-    constexpr int kUnits = (L::kCols / 8 + 3) / 4;
-    float acc[kUnits][2 * R][4];
+    };
+    // ---- k S0 and q S0, a warp's tiles of eight columns for all rows: the right-hand sides and the start of the read-out ----
+    auto state_products = [&] {
+        for (int tile = tile0; tile < tiles; tile += kStride) {
+            float acc[2 * R][4];
 #pragma unroll
-    for (int un = 0; un < kUnits; ++un) {
-        const int tile = tile0 + 4 * un;
-        if (tile >= tiles) break;
-        if (un) load(tile, s);
+            for (int m = 0; m < 2 * R; ++m)
 #pragma unroll
-        for (int m = 0; m < 2 * R; ++m)
+                for (int x = 0; x < 4; ++x) acc[m][x] = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) acc[un][m][x] = 0.f;
+            for (int k = 0; k < kKs; ++k) {
+                uint32_t b0[3], b1[3], af[2 * R][4];
+                split3(s[k][0], s[k][1], b0);
+                split3(s[k][2], s[k][3], b1);
+                if (tile + kStride < tiles) load(tile + kStride, k, s[k]);
 #pragma unroll
-        for (int k = 0; k < kKs; ++k) {
-            uint32_t b0[3], b1[3];
-            split3(s[k][0], s[k][1], b0);
-            split3(s[k][2], s[k][3], b1);
+                for (int m = 0; m < 2 * R; ++m)
+                    ldmatrix_x4((m < R ? k_at : q_at) + ((m % R) * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af[m]);
 #pragma unroll
-            for (int m = 0; m < 2 * R; ++m) {
-                uint32_t af[4];
-                ldmatrix_x4((m < R ? k_at : q_at) + ((m % R) * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af);
+                for (int x = 2; x >= 0; --x)
 #pragma unroll
-                for (int x = 2; x >= 0; --x) mma_bf16(acc[un][m], af, b0[x], b1[x]);
+                    for (int m = 0; m < 2 * R; ++m) mma_bf16(acc[m], af[m], b0[x], b1[x]);
             }
-        }
-    }
-    sync();                                       // k has been read: the right-hand sides take its place
+            const int at = tile * 8 + 2 * c4;
 #pragma unroll
-    for (int un = 0; un < kUnits; ++un) {
-        const int tile = tile0 + 4 * un, at = tile * 8 + 2 * c4;
-        if (tile >= tiles) break;
+            for (int m = 0; m < 2 * R; ++m)
 #pragma unroll
-        for (int m = 0; m < 2 * R; ++m)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int t = (m % R) * 16 + r * 8 + g4;
-                const float x0 = acc[un][m][2 * r], x1 = acc[un][m][2 * r + 1];
-                if (m < R) {
-                    const float fk = nd->whole[t] * rk_la(t), bt = nd->beta[t];
-                    const float2 v = bf2(*reinterpret_cast<const uint32_t *>(sm + L::oV + t * L::kPitchV + at * 2));
-                    *reinterpret_cast<float2 *>(su + t * cols + at) =
-                        t < n ? make_float2(bt * (v.x - fk * x0), bt * (v.y - fk * x1)) : make_float2(0.f, 0.f);
-                } else {
-                    const float fq = a.scale_la * nd->whole[t] * rq_la(t);
-                    *reinterpret_cast<float2 *>(so + t * cols + at) = make_float2(fq * x0, fq * x1);
+                for (int r = 0; r < 2; ++r) {
+                    const int t = (m % R) * 16 + r * 8 + g4;
+                    const float x0 = acc[m][2 * r], x1 = acc[m][2 * r + 1];
+                    if (m < R) {
+                        const float fk = nd->whole[t] * rk_la(t), bt = nd->beta[t];
+                        const float2 v = bf2(*reinterpret_cast<const uint32_t *>(sm + L::oV + t * L::kPitchV + at * 2));
+                        *reinterpret_cast<float2 *>(su + t * cols + at) =
+                            t < n ? make_float2(bt * (v.x - fk * x0), bt * (v.y - fk * x1)) : make_float2(0.f, 0.f);
+                    } else {
+                        const float fq = a.scale_la * nd->whole[t] * rq_la(t);
+                        *reinterpret_cast<float2 *>(so + t * cols + at) = make_float2(fq * x0, fq * x1);
+                    }
                 }
-            }
-    }
-    sync();
+        }
+    };
+    if (warp < R) tables();
+    if (!kApart || warp >= R) state_products();
+    sync();                                       // (k has been read: the sums over the tree's V take its place)
     // ---- the substitution: a thread's column, by blocks of 16 nodes.  A node that u_j does not reach has a zero in the table; a
     // block in which something is not finite is done again, along the paths. ----
     if (tid < cols) {
@@ -594,22 +580,39 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
             }
         }
     }
+    // ---- the sums over the tree's V, by the warps that the substitution leaves.  (Here and below a row's own non-finite entries
+    // spoil that row alone; those of V and u are taken as zeros and added afterwards to the rows that see them.) ----
+    constexpr int kSums = kWarps == 4 ? 2 : 4;    // these warps (64 columns keep two busy with the substitution)
+    if (warp >= kWarps - kSums)
+        for (int item = warp - (kWarps - kSums); item < R * tiles; item += kSums) {
+            const int m = item % R, tile = item / R;
+            float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (k > m) break;                 // (parents come first)
+                uint32_t af[4], bf[2];
+                ldmatrix_x4(tc::smem_u32(sm + L::oP) + (m * 16 + (lane & 15)) * L::kPitchP + (2 * k + (lane >> 4)) * 16, af);
+                ldmatrix_x2_trans(v_at + (k * 16 + (lane & 15)) * L::kPitchV + tile * 16, bf);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if ((bf[x] & 0x7f80u) == 0x7f80u) bf[x] &= 0xffff0000u;
+                    if ((bf[x] & 0x7f800000u) == 0x7f800000u) bf[x] &= 0xffffu;
+                }
+                mma_bf16(o, af, bf[0], bf[1]);
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                *reinterpret_cast<float2 *>(st + (m * 16 + r * 8 + g4) * cols + tile * 8 + 2 * c4) = make_float2(o[2 * r], o[2 * r + 1]);
+        }
     if (odd) s_odd = 1;
     sync();
     odd = s_odd != 0;
-    if (a.u)
-        for (int i = tid; i < n * (cols / 4); i += kHalf) {
-            const int t = i / (cols / 4), c = (i - t * (cols / 4)) * 4;
-            *reinterpret_cast<float4 *>(a.u + (((size_t)b * T + t) * a.H + h) * D + c0 + c) =
-                *reinterpret_cast<const float4 *>(su + t * cols + c);
-        }
-    // ---- the read-outs.  (A row's own non-finite entries spoil that row alone; those of u and V are taken as zeros here and
-    // added below to the rows that see them.) ----
-    auto clean = [&](float x) { return odd && !finite(x) ? 0.f : x; };
+    // ---- the linear read-out ----
     if (warp < R) {
+        auto clean = [&](float x) { return odd && !finite(x) ? 0.f : x; };
         for (int tile = 0; tile < tiles; ++tile) {
             const int at = tile * 8 + 2 * c4;
-            float o[4];
+            float o[4], lo[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const float2 y = *reinterpret_cast<const float2 *>(so + (warp * 16 + r * 8 + g4) * cols + at);
@@ -618,83 +621,59 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
             }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
-                if (k > warp) break;              // (parents come first)
+                if (k > warp) break;
                 const float *y = su + (k * 16 + 2 * c4) * cols + tile * 8 + g4;
                 uint32_t b0[2], b1[2];
                 split2(clean(y[0]), clean(y[cols]), b0);
                 split2(clean(y[8 * cols]), clean(y[9 * cols]), b1);
-                mma_bf16(o, bl_f[k], b0[0], b1[0]);
-                mma_bf16(o, bh_f[k], b0[1], b1[1]);
+                mma_bf16(lo, bl_f[k], b0[0], b1[0]);
                 mma_bf16(o, bh_f[k], b0[0], b1[0]);
+                mma_bf16(lo, bh_f[k], b0[1], b1[1]);
             }
 #pragma unroll
             for (int r = 0; r < 2; ++r)
-                *reinterpret_cast<float2 *>(so + (warp * 16 + r * 8 + g4) * cols + at) = make_float2(o[2 * r], o[2 * r + 1]);
+                *reinterpret_cast<float2 *>(so + (warp * 16 + r * 8 + g4) * cols + at) = make_float2(o[2 * r] + lo[2 * r], o[2 * r + 1] + lo[2 * r + 1]);
         }
     }
-    // x (hi + lo) of the A fragments, as a table [t][j] in the table's place
-    auto dump = [&](const uint32_t (&hi)[kNt / 2][4], const uint32_t (&lo)[kNt / 2][4], bool both) {
+    if (a.u)
+        for (int i = kHalf - 1 - tid; i < n * (cols / 4); i += kHalf) {      // (the last warps first)
+            const int t = i / (cols / 4), c = (i - t * (cols / 4)) * 4;
+            *reinterpret_cast<float4 *>(a.u + (((size_t)b * T + t) * a.H + h) * D + c0 + c) =
+                *reinterpret_cast<const float4 *>(su + t * cols + c);
+        }
+    if (odd) {
         sync();
-        if (warp < R)
+        if (warp < R)                             // what the read-out takes from u, in the table's place, [t][j]
 #pragma unroll
             for (int k = 0; k < kNt / 2; ++k)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float2 y = bf2(hi[k][x]), w = both ? bf2(lo[k][x]) : make_float2(0.f, 0.f);
+                    const float2 y = bf2(bh_f[k][x]), w = bf2(bl_f[k][x]);
                     float *to = tab + (warp * 16 + (x & 1) * 8 + g4) * kRows + k * 16 + (x >> 1) * 8 + 2 * c4;
                     to[0] = y.x + w.x;
                     to[1] = y.y + w.y;
                 }
         sync();
-    };
-    if (odd) {
-        dump(bh_f, bl_f, true);
         for (int i = tid; i < n * cols; i += kHalf) {
             const int t = i / cols, c = i - t * cols;
-            for (unsigned long long w = (nd->above[t] | 1ull << t) & nd->fold; w; w &= w - 1) {
+            const unsigned long long path = nd->above[t] | 1ull << t;
+            for (unsigned long long w = path & nd->fold; w; w &= w - 1) {
                 const int j = __ffsll(w) - 1;
                 if (!finite(su[j * cols + c])) so[i] += tab[t * kRows + j] * su[j * cols + c];
             }
-        }
-        dump(p_f, p_f, false);
-    }
-    if (warp < R) {
-        for (int tile = 0; tile < tiles; ++tile) {
-            float o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                if (k > warp) break;
-                uint32_t bf[2];
-                ldmatrix_x2_trans(v_at + (k * 16 + (lane & 15)) * L::kPitchV + tile * 16, bf);
-                if (odd)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if ((bf[x] & 0x7f80u) == 0x7f80u) bf[x] &= 0xffff0000u;
-                        if ((bf[x] & 0x7f800000u) == 0x7f800000u) bf[x] &= 0xffffu;
-                    }
-                mma_bf16(o, p_f[k], bf[0], bf[1]);
-            }
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                *reinterpret_cast<float2 *>(st + (warp * 16 + r * 8 + g4) * cols + tile * 8 + 2 * c4) = make_float2(o[2 * r], o[2 * r + 1]);
-        }
-    }
-    if (odd) {
-        sync();
-        for (int i = tid; i < n * cols; i += kHalf) {
-            const int t = i / cols, c = i - t * cols;
-            for (unsigned long long w = (nd->above[t] | 1ull << t) & nd->keep; w; w &= w - 1) {
+            for (unsigned long long w = path & nd->keep; w; w &= w - 1) {
                 const int j = __ffsll(w) - 1;
                 const float v = to_f32(*reinterpret_cast<const __nv_bfloat16 *>(sm + L::oV + j * L::kPitchV + c * 2));
-                if (!finite(v)) st[i] += tab[t * kRows + j] * v;
+                if (!finite(v)) st[i] += to_f32(*reinterpret_cast<const __nv_bfloat16 *>(sm + L::oP + t * L::kPitchP + j * 2)) * v;
             }
         }
     }
 }
 
 template <int D, int G, bool kNorm, int R>
-__global__ void __launch_bounds__(kThreads, Layout<D, R>::kCtas) tree_tc_kernel(Args a) {
+__global__ void __launch_bounds__(Layout<D, R>::kThreads, Layout<D, R>::kCtas) tree_tc_kernel(Args a) {
     using L = Layout<D, R>;
+    constexpr int kHalf = L::kHalf, kThreads = L::kThreads;
     extern __shared__ __align__(128) uint8_t dyn_tc[];
     __shared__ typename L::N nodes;
     const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, tid = threadIdx.x;
@@ -737,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, R>::kCtas) tree_tc_kernel(
     if (tid < kHalf) cache_part<D, G, kNorm, R>(a, sums, dyn_tc, in, n);
     else tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank, odd, node);
     join_rows<__nv_bfloat16, D>(a, b, h, n, rank, sums, reinterpret_cast<const float *>(dyn_tc + L::oRing), L::kAccPitch,
-                                reinterpret_cast<const float *>(dyn_tc + L::oO), reinterpret_cast<const float *>(dyn_tc + L::oT));
+                                reinterpret_cast<const float *>(dyn_tc + L::oO), reinterpret_cast<const float *>(dyn_tc + L::oK));
 }
 
 template <int D, int G, bool kNorm, int R>
@@ -745,7 +724,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     auto kernel = tree_tc_kernel<D, G, kNorm, R>;
     cudaError_t e = allow_smem(kernel, Layout<D, R>::kTotal);
     if (e != cudaSuccess) return e;
-    return launch_clusters(kernel, a, BH, kThreads, Layout<D, R>::kTotal, st);
+    return launch_clusters(kernel, a, BH, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st);
 }
 template <int D, int G, bool kNorm>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
