@@ -82,9 +82,9 @@ bool generation_groups(const natsl_params *p) {
     const int G = head_groups(p).G;
     return G == 1 || ((G == 2 || G == 4) && p->d / G >= 32);
 }
-// A cache's rows, and blocks of them over all pairs, are counted in 31 bits.
+// The rows of all caches are counted in 31 bits (of the smallest they would be 2 x 275 GB).
 bool cache_fits(const natsl_params *p, int32_t cap) {
-    return cap > 0 && (long long)p->B * p->H <= 0x7fffffff / 65 && (long long)p->B * p->H * ((cap + 15LL) / 16) <= 0x7fffffff;
+    return cap > 0 && (long long)p->B * p->H <= 0x7fffffff / 8 && (long long)p->B * p->H * cap <= 0x7fffffff;
 }
 
 bool use_tensor_cores(const natsl_params *p) {

@@ -155,69 +155,88 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
     constexpr int V = D / 32, cols = D / kCluster;
     const int lane = threadIdx.x & 31, G = a.G, ls = 32 / G, sg = lane / ls, step = kCluster * (blockDim.x >> 5);
     const int owner = lane * V / cols, at = lane * V - owner * cols;
-    int t = rank + kCluster * (threadIdx.x >> 5);
-    float2 w = make_float2(0.5f, 0.5f), w_next = w;
-    auto weights = [&](int t) { return *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t) * a.H + h) * 2); };
-    if (a.w && t < n) w_next = weights(t);
-    cluster_arrive();
-    cluster_wait();
-    bool read = false;
-    for (; t < n; t += step) {
-        w = w_next;
-        if (a.w && t + step < n) w_next = weights(t + step);
-        float m[kCluster], z[kCluster], x[kCluster][V], o[V], ol[V];
+    struct Row {
+        float m[kCluster], z[kCluster], x[kCluster][V], mt, zt, o[V], la[V];
+        float2 w;
+    };
+    auto weights = [&](int t) {
+        return a.w ? *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t) * a.H + h) * 2) : make_float2(0.5f, 0.5f);
+    };
+    auto load = [&](int t, Row &y) {
 #pragma unroll
         for (int r = 0; r < kCluster; ++r) {
-            m[r] = ld_remote(remote(&sums->cache_m[sg][t], r));
-            z[r] = ld_remote(remote(&sums->cache_z[sg][t], r));
-            ld_remote<V>(remote(acc + t * acc_pitch + lane * V, r), x[r]);
+            y.m[r] = ld_remote(remote(&sums->cache_m[sg][t], r));
+            y.z[r] = ld_remote(remote(&sums->cache_z[sg][t], r));
+            ld_remote<V>(remote(acc + t * acc_pitch + lane * V, r), y.x[r]);
         }
-        const float mt = ld_remote(remote(&sums->tree_m[sg][t], owner)), zt = ld_remote(remote(&sums->tree_z[sg][t], owner));
-        ld_remote<V>(remote(o_tree + t * cols + at, owner), o);
-        ld_remote<V>(remote(o_la + t * cols + at, owner), ol);
-        float M = mt;
+        y.mt = ld_remote(remote(&sums->tree_m[sg][t], owner));
+        y.zt = ld_remote(remote(&sums->tree_z[sg][t], owner));
+        ld_remote<V>(remote(o_tree + t * cols + at, owner), y.o);
+        ld_remote<V>(remote(o_la + t * cols + at, owner), y.la);
+    };
+    auto finish = [&](int t, Row &y, bool last) {
+        float M = y.mt;
 #pragma unroll
-        for (int r = 0; r < kCluster; ++r) M = fmaxf(M, m[r]);
-        const float Mu = M == -INFINITY ? 0.f : M, ft = tc::ex2_ftz(mt - Mu);
-        float Z = zt * ft;
+        for (int r = 0; r < kCluster; ++r) M = fmaxf(M, y.m[r]);
+        const float Mu = M == -INFINITY ? 0.f : M, ft = tc::ex2_ftz(y.mt - Mu);
+        float Z = y.zt * ft;
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] *= ft;
+        for (int i = 0; i < V; ++i) y.o[i] *= ft;
 #pragma unroll
         for (int r = 0; r < kCluster; ++r) {
-            const float f = tc::ex2_ftz(m[r] - Mu);
-            Z = fmaf(z[r], f, Z);
+            const float f = tc::ex2_ftz(y.m[r] - Mu);
+            Z = fmaf(y.z[r], f, Z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = fmaf(x[r][i], f, o[i]);
+            for (int i = 0; i < V; ++i) y.o[i] = fmaf(y.x[r][i], f, y.o[i]);
         }
         const float iz = Z == 0.f ? 0.f : 1.f / Z;     // (no visible key: o_nla = 0)
         float sn = 0.f, sl = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            o[i] *= iz;
-            sn = fmaf(o[i], o[i], sn);
-            sl = fmaf(ol[i], ol[i], sl);
+            y.o[i] *= iz;
+            sn = fmaf(y.o[i], y.o[i], sn);
+            sl = fmaf(y.la[i], y.la[i], sl);
         }
+        if (last) cluster_arrive();               // (the warp has read its last row)
         for (int s = ls / 2; s > 0; s >>= 1) sn += __shfl_xor_sync(0xffffffffu, sn, s);
         sl = warp_sum(sl);
-        const float fn = w.x * rsqrtf(sn / (D / G) + a.eps), fl = w.y * rsqrtf(sl / D + a.eps);
+        const float fn = y.w.x * rsqrtf(sn / (D / G) + a.eps), fl = y.w.y * rsqrtf(sl / D + a.eps);
         ST *out = reinterpret_cast<ST *>(a.out) + (((size_t)b * a.T + t) * a.H + h) * D + lane * V;
-        float y[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = fmaf(fn, o[i], fl * ol[i]);
+        for (int i = 0; i < V; ++i) y.o[i] = fmaf(fn, y.o[i], fl * y.la[i]);
         if constexpr (V == 4) {
-            store4(out, make_float4(y[0], y[1], y[2], y[3]));
+            store4(out, make_float4(y.o[0], y.o[1], y.o[2], y.o[3]));
         } else {
-            out[0] = from_f32<ST>(y[0]);
-            out[1] = from_f32<ST>(y[1]);
-        }
-        if (t + step >= n) {                      // (the warp's last row has arrived)
-            cluster_arrive();
-            read = true;
+            out[0] = from_f32<ST>(y.o[0]);
+            out[1] = from_f32<ST>(y.o[1]);
         }
         if (a.lse && lane % ls == 0)
             a.lse[(((size_t)b * a.H + h) * G + sg) * a.T + t] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * kLn2;
+    };
+    int t = rank + kCluster * (threadIdx.x >> 5);
+    Row y;
+    y.w = t < n ? weights(t) : make_float2(0.f, 0.f);
+    cluster_arrive();
+    cluster_wait();
+    if (t >= n) cluster_arrive();                 // (no row for this warp)
+    else load(t, y);
+    for (; t < n; t += step) {                    // (with two CTAs, where rows are many, a row is on its way while one is finished)
+        if constexpr (kCluster == 2) {
+            Row next;
+            if (t + step < n) {
+                next.w = weights(t + step);
+                load(t + step, next);
+            }
+            finish(t, y, t + step >= n);
+            y = next;
+        } else {
+            finish(t, y, t + step >= n);
+            if (t + step < n) {
+                y.w = weights(t + step);
+                load(t + step, y);
+            }
+        }
     }
-    if (!read) cluster_arrive();
     cluster_wait();                               // nobody's shared memory goes while a neighbour still reads it
 }
 template <typename ST, int D, typename S>
@@ -228,23 +247,23 @@ __device__ __forceinline__ void join_rows(const Args &a, int b, int h, int n, in
     else join_rows_of<ST, D, 8>(a, b, h, n, rank, sums, acc, acc_pitch, o_la, o_tree);
 }
 
-// One cluster per pair.
-template <typename K, typename... More>
-cudaError_t launch_clusters(K kernel, const Args &a, int BH, int threads, size_t smem, cudaStream_t st, More... more) {
+// One cluster per pair, placed while the work before it in the stream finishes.
+template <typename K, typename... A>
+cudaError_t launch_clusters(K kernel, int grid, int cluster, int threads, size_t smem, cudaStream_t st, const A &...args) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(BH * a.cluster);
+    cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = a.cluster;
+    attr[0].val.clusterDim.x = cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // (placed while the work before it finishes)
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a, more...);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
     count_launch();
     return e;
 }

@@ -341,7 +341,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     const int bytes = 4 * (fixed + (beside ? tree + cache : std::max(tree, cache)));
     cudaError_t e = allow_smem(tree_simt_kernel<ST, D, TT>, kMost);
     if (e != cudaSuccess) return e;
-    return launch_clusters(tree_simt_kernel<ST, D, TT>, a, BH, kThreads, bytes, st, beside);
+    return launch_clusters(tree_simt_kernel<ST, D, TT>, BH * a.cluster, a.cluster, kThreads, bytes, st, a, beside);
 }
 template <typename ST, int D>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {

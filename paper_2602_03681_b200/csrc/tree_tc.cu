@@ -349,10 +349,8 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = __ldg(S + (size_t)(16 * k + 2 * c4 + (i & 1) + (i >> 1) * 8) * D + tile * 8);
     };
-    // (the first warps have the tables; beyond 32 nodes that is all they do meanwhile)
-    constexpr bool kApart = R == 4;
-    constexpr int kStride = kApart ? kWarps - R : kWarps;
-    const int tiles = cols / 8, tile0 = kApart && warp < R ? tiles : kWarps - 1 - warp;
+    const int tiles = cols / 8, tile0 = warp < R ? tiles : kWarps - 1 - warp;       // (the first R warps have the tables)
+    constexpr int kStride = kWarps - R;
     float s[kKs][4];
     if (tile0 < tiles)
 #pragma unroll
@@ -406,7 +404,7 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
             total[r] = nd->total[t];
             wipes[r] = nd->wipes[t];
         }
-        constexpr int kPart = kNt < 4 ? kNt : 4;  // (32 columns at a time: registers)
+        constexpr int kPart = 2;                  // (16 columns at a time: registers)
 #pragma unroll
         for (int i0 = 0; i0 < kNt; i0 += kPart) {
             float kk[kPart][4], qk[G][kPart][4];
@@ -496,17 +494,22 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                 for (int x = 0; x < 4; ++x) acc[m][x] = 0.f;
 #pragma unroll
             for (int k = 0; k < kKs; ++k) {
-                uint32_t b0[3], b1[3], af[2 * R][4];
+                uint32_t b0[3], b1[3];
                 split3(s[k][0], s[k][1], b0);
                 split3(s[k][2], s[k][3], b1);
                 if (tile + kStride < tiles) load(tile + kStride, k, s[k]);
+                constexpr int kM = R == 4 ? 4 : 2 * R;       // (row tiles at a time: registers)
 #pragma unroll
-                for (int m = 0; m < 2 * R; ++m)
-                    ldmatrix_x4((m < R ? k_at : q_at) + ((m % R) * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af[m]);
+                for (int m0 = 0; m0 < 2 * R; m0 += kM) {
+                    uint32_t af[kM][4];
 #pragma unroll
-                for (int x = 2; x >= 0; --x)
+                    for (int m = 0; m < kM; ++m)
+                        ldmatrix_x4((m0 + m < R ? k_at : q_at) + ((m0 + m) % R * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af[m]);
 #pragma unroll
-                    for (int m = 0; m < 2 * R; ++m) mma_bf16(acc[m], af[m], b0[x], b1[x]);
+                    for (int x = 2; x >= 0; --x)
+#pragma unroll
+                        for (int m = 0; m < kM; ++m) mma_bf16(acc[m0 + m], af[m], b0[x], b1[x]);
+                }
             }
             const int at = tile * 8 + 2 * c4;
 #pragma unroll
@@ -528,7 +531,7 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
         }
     };
     if (warp < R) tables();
-    if (!kApart || warp >= R) state_products();
+    else state_products();
     sync();                                       // (k has been read: the sums over the tree's V take its place)
     // ---- the substitution: a thread's column, by blocks of 16 nodes.  A node that u_j does not reach has a zero in the table; a
     // block in which something is not finite is done again, along the paths. ----
@@ -724,7 +727,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     auto kernel = tree_tc_kernel<D, G, kNorm, R>;
     cudaError_t e = allow_smem(kernel, Layout<D, R>::kTotal);
     if (e != cudaSuccess) return e;
-    return launch_clusters(kernel, a, BH, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st);
+    return launch_clusters(kernel, BH * a.cluster, a.cluster, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st, a);
 }
 template <int D, int G, bool kNorm>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
