@@ -4,12 +4,13 @@
 //   weight_j += sum_t sum_s exp(scale q_ts.k_js - lse_ts)   over the rows that see it,
 // from the log-sum-exps that the attention itself has left, so K is read once and V not at all.
 //
-// natsl_cache_evict keeps the first entries, the latest ones and the heaviest of the rest (a bisection on the weights'
-// bits finds the threshold; ties to the lowest index) and moves them to the front, in order and in place.
+// natsl_cache_evict keeps the first entries, the latest ones and the heaviest of the rest (a radix select on the
+// weights' bits finds the threshold; ties to the lowest index) and moves them to the front, in order and in place.
 #include <algorithm>
 #include "common.cuh"
 #include "natsl_internal.h"
 #include "tc_common.cuh"
+#include "tree_common.cuh"
 
 namespace natsl {
 namespace {
@@ -122,6 +123,7 @@ cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__
     extern __shared__ __align__(128) uint8_t dyn_w[];      // the ring; then the sums [row groups][run]
     __shared__ float2 s_row[G][kRows];            // factor to base-2 logits, log-sum-exp in base 2
     __shared__ int s_vis[G][kRows];
+    __shared__ __align__(8) float s_key[kNorm ? G : 1][kTTile];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
     const int rg = warp / kKeyGroups, kg = warp - rg * kKeyGroups, r0 = rg * 16 * kMt;
     const int bh = blockIdx.x / runs, b = bh / H, h = bh - b * H, n = min(max(cache_len[bh], 0), cap);
@@ -197,25 +199,46 @@ cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__
                         f[g][m][r].x *= rsqrtf(ss / ds + norm_eps);
                     }
                 }
+        int least = 0x7fffffff;                   // keys that all of the warp's rows see
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) least = min(least, vis[g][m][r]);
+        least = __reduce_min_sync(0xffffffffu, least + 2 * c4);
         for (int t = 0; t < tiles; ++t) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kTStages - 2) : "memory");
             __syncthreads();                      // tile t is there, and every warp is done with tile t - 1 ...
             fetch(t + kTStages - 1);              // ... whose place this one takes
             const uint32_t kt = ring + t % kTStages * kTileBytes;
+            if (kNorm) {                          // a key's RMS factors: two threads each, half a row
+                const int key = tid >> 1, half = tid & 1;
+                const uint8_t *row = dyn_w + (kt - ring) + key * kRowBytes;
+                float ss = 0.f;
+#pragma unroll
+                for (int i = 0; i < kPieces / 2; ++i) {
+                    const int p = half * (kPieces / 2) + ((i + 4 * half) & (kPieces / 2 - 1));
+                    const uint4 y = *reinterpret_cast<const uint4 *>(row + ((p ^ (key & 7)) << 4));
+                    ss = square_sum(y.x, square_sum(y.y, square_sum(y.z, square_sum(y.w, ss))));
+                }
+                if (G == 1) ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+                s_key[G == 2 ? half : 0][key] = rsqrtf(ss / ds + norm_eps);
+                __syncthreads();
+            }
             float sum[kNt][2];
 #pragma unroll
             for (int i = 0; i < kNt; ++i) sum[i][0] = sum[i][1] = 0.f;
+            const bool all = (t + 1) * kTTile <= least;      // (uniform)
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                float x[kMt][kNt][4], kk[kNt];
+                float x[kMt][kNt][4];
 #pragma unroll
-                for (int i = 0; i < kNt; ++i) {
-                    kk[i] = 0.f;
+                for (int i = 0; i < kNt; ++i)
 #pragma unroll
                     for (int m = 0; m < kMt; ++m)
 #pragma unroll
                         for (int y = 0; y < 4; ++y) x[m][i][y] = 0.f;
-                }
 #pragma unroll
                 for (int k = g * kKs; k < (g + 1) * kKs; ++k)
 #pragma unroll
@@ -228,32 +251,40 @@ cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__
                             mma_bf16(x[m][i], qf[m][k], bf[0], bf[1]);
                             mma_bf16(x[m][i + 1], qf[m][k], bf[2], bf[3]);
                         }
-                        if (kNorm) {
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) kk[i + y / 2] = square_sum(bf[y], kk[i + y / 2]);
-                        }
                     }
 #pragma unroll
                 for (int i = 0; i < kNt; ++i) {
-                    float w[2] = {1.f, 1.f};
-                    if (kNorm) {                  // (a lane's sum of squares belongs to key g4 of tile i, its columns to 2 c4, + 1)
-                        kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 1);
-                        kk[i] += __shfl_xor_sync(0xffffffffu, kk[i], 2);
-                        const float y = rsqrtf(fmaf(kk[i], 1.f / ds, norm_eps));
-                        w[0] = __shfl_sync(0xffffffffu, y, c4 * 8);
-                        w[1] = __shfl_sync(0xffffffffu, y, c4 * 8 + 4);
-                    }
+                    float2 w = make_float2(1.f, 1.f);
+                    if (kNorm) w = *reinterpret_cast<const float2 *>(&s_key[g][kg * kKeys + i * 8 + 2 * c4]);
 #pragma unroll
                     for (int m = 0; m < kMt; ++m)
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
-                                const float z = kNorm ? x[m][i][2 * r + y] * w[y] : x[m][i][2 * r + y];
-                                const float e = tc::ex2_ftz(fmaf(z, f[g][m][r].x, -f[g][m][r].y));
-                                sum[i][y] += t * kTTile + i * 8 + y < vis[g][m][r] ? e : 0.f;
+                                const float z = kNorm ? x[m][i][2 * r + y] * (y ? w.y : w.x) : x[m][i][2 * r + y];
+                                x[m][i][2 * r + y] = tc::ex2_ftz(fmaf(z, f[g][m][r].x, -f[g][m][r].y));
                             }
                 }
+                if (!all)
+#pragma unroll
+                    for (int i = 0; i < kNt; ++i)
+#pragma unroll
+                        for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                                for (int y = 0; y < 2; ++y)
+                                    if (t * kTTile + i * 8 + y >= vis[g][m][r]) x[m][i][2 * r + y] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kNt; ++i)
+#pragma unroll
+                    for (int m = 0; m < kMt; ++m)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            sum[i][0] += x[m][i][2 * r];
+                            sum[i][1] += x[m][i][2 * r + 1];
+                        }
             }
 #pragma unroll
             for (int i = 0; i < kNt; ++i)
@@ -298,12 +329,12 @@ cudaError_t launch_weights_tc(const void *q, const float *lse, const int32_t *vi
 }
 
 // ------------------------------------------------------------------------------------------
-// Eviction.  Every CTA of a pair's cluster finds out what stays (all of them the same: that costs no time, and nobody waits for
-// a list), then they move the rows in waves: a wave of rows is read into shared memory by the CTAs, and written behind the
+// Eviction.  A pair is the work of one CTA, or of a cluster where pairs are few: its CTAs share the entries to find what stays and
+// list it, then they move the rows in waves: a wave of rows is read into shared memory by the CTAs, and written behind the
 // cluster's barrier.  Entry r comes from kept[r] >= r, so what a wave writes lies below everything that later waves read.  And
 // once one entry is gone all behind it move: what lies before the first gap is left in place.
 // ------------------------------------------------------------------------------------------
-constexpr int kEThreads = 512, kEWarps = kEThreads / 32;
+constexpr int kEThreads = 512, kEWarps = kEThreads / 32, kBins = 256;
 
 // Weights in the order of unsigned words: a NaN below everything (0), both zeros equal.
 __device__ __forceinline__ uint32_t order_key(float w) {
@@ -312,14 +343,15 @@ __device__ __forceinline__ uint32_t order_key(float w) {
     return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-// kHeld: entries per lane whose keys stay in registers (512 kHeld per pair); more lie in shared memory where the rows will be,
-// and what does not fit there is read again.
+// kHeld: entries per lane whose keys stay in registers (512 kHeld per CTA); more lie in shared memory where the rows will be, and
+// what does not fit there is read again.
 template <int kRowBytes, int kHeld>
 __global__ void __launch_bounds__(kEThreads)
 evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first, int recent,
              int32_t *kept, int cluster, int rows) {
     extern __shared__ __align__(16) uint8_t dyn_e[];       // [2][rows][kRowBytes], then the rows' weights and sources
-    __shared__ int s_warp[2][kEWarps], s_count[2][kEWarps], s_gap;
+    __shared__ int hist[2][kBins], s_warp[2][kEWarps], s_pick[2], s_total[2], s_gap;
+    __shared__ uint32_t s_all, s_any;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x / cluster, rank = blockIdx.x - bh * cluster;
     float *w = weight + (size_t)bh * cap;
     int32_t *list = kept + (size_t)bh * keep;
@@ -328,10 +360,16 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
         for (int i = rank * kEThreads + tid; i < n; i += cluster * kEThreads) list[i] = i;
         return;
     }
-    // ---- a warp owns a run of entries, a lane every 32nd of them.  Candidates have their key; what is safe anyway, or no entry,
-    // has 0, which no count below takes in. ----
+    auto meet = [&] {                             // the cluster's barrier
+        if (cluster > 1) { tree::cluster_arrive(); tree::cluster_wait(); }
+        else __syncthreads();
+    };
+    auto of_rank = [&](const void *p, int r) { return __float_as_int(tree::ld_remote(tree::remote(p, r))); };
+    if (tid == 0) { s_all = 0xffffffffu; s_any = 0u; s_gap = keep; }
+    // ---- a warp owns a run of entries, a lane every 32nd of them ----
     const int lo = first, hi = n - recent, want = keep - first - recent;      // candidates; how many of them stay
-    const int run = ((n + kEWarps - 1) / kEWarps + 31) / 32 * 32, j0 = min(n, warp * run), j1 = min(n, j0 + run), steps = (j1 - j0 + 31) / 32;
+    const int warps = cluster * kEWarps, run = ((n + warps - 1) / warps + 31) / 32 * 32;
+    const int j0 = (int)min((long long)n, (long long)(rank * kEWarps + warp) * run), j1 = min(n, j0 + run), steps = (j1 - j0 + 31) / 32;
     auto is_candidate = [&](int j) { return (j < j1) & (j >= lo) & (j < hi); };
     auto key_of = [&](int j) { return is_candidate(j) ? order_key(w[j]) : 0u; };
     uint32_t held[kHeld];
@@ -348,10 +386,12 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
             f(j, i < kHeld + spare ? more[(i - kHeld) * 32] : key_of(j));
         }
     };
-    // ---- the threshold, bit by bit from the highest in which two candidates differ: is what has it set enough?  (Histograms of
-    // the leading bits meet in a few bins: 57 us a call at 16 pairs of 8192.) ----
-    int need = 0;
+    // ---- the threshold, eight bits at a time from the highest in which two candidates differ: a histogram in each CTA, summed by
+    // all of them over distributed shared memory.  (From the first bit on, weights meet in a few bins and their counters queue;
+    // a bit at a time, over all of a pair's entries in each CTA, took 23 of a call's 34 us at 16 pairs of 8192.) ----
+    int need = want;
     uint32_t prefix = 0xffffffffu;                // (nothing is over it or equal to it where nothing more is wanted)
+    __syncthreads();
     if (want > 0) {
         uint32_t all = 0xffffffffu, any = 0u;
         each([&](int j, uint32_t x) {
@@ -360,26 +400,41 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
         });
         all = __reduce_and_sync(0xffffffffu, all);
         any = __reduce_or_sync(0xffffffffu, any);
-        if (lane == 0) { s_warp[0][warp] = (int)all; s_warp[1][warp] = (int)any; }
-        __syncthreads();
-        all = __reduce_and_sync(0xffffffffu, (uint32_t)s_warp[0][lane % kEWarps]);
-        any = __reduce_or_sync(0xffffffffu, (uint32_t)s_warp[1][lane % kEWarps]);
+        if (lane == 0) { atomicAnd(&s_all, all); atomicOr(&s_any, any); }
+        meet();
+        all = __reduce_and_sync(0xffffffffu, lane < cluster ? (uint32_t)of_rank(&s_all, lane) : 0xffffffffu);
+        any = __reduce_or_sync(0xffffffffu, lane < cluster ? (uint32_t)of_rank(&s_any, lane) : 0u);
         const int top = 31 - __clz((int)(all ^ any));                          // (-1: all alike)
         prefix = top < 0 ? all : top == 31 ? 0u : all & ~((2u << top) - 1u);
-        auto count = [&](uint32_t x0, int set) {  // candidates with keys >= x0 > 0; two sets of counts: one barrier a count
-            int c = 0;
-            each([&](int, uint32_t x) { c += x >= x0; });
-            c = __reduce_add_sync(0xffffffffu, c);
-            if (lane == 0) s_count[set][warp] = c;
+        for (int above = top + 1, set = 0; above > 0; set ^= 1) {              // bits from `above` on are found
+            const int shift = max(0, above - 8);
+            if (tid < kBins) hist[set][tid] = 0;
             __syncthreads();
-            return __reduce_add_sync(0xffffffffu, lane < kEWarps ? s_count[set][lane] : 0);
-        };
-        for (int bit = top; bit >= 0; --bit)
-            if (count(prefix | 1u << bit, bit & 1) >= want) prefix |= 1u << bit;
-        need = want;
-        if (prefix != 0xffffffffu) {              // (uniform)
+            each([&](int j, uint32_t x) {
+                const bool in = is_candidate(j) & ((above < 32 ? (x ^ prefix) >> above : 0u) == 0u);
+                if (in) atomicAdd(&hist[set][x >> shift & (above - shift < 8 ? (1u << (above - shift)) - 1u : 255u)], 1);
+            });
+            meet();                               // (a set is filled again two passes on: whoever does has seen everyone read it)
+            int c = 0, sum = 0;
+            if (tid < kBins) {                    // thread i: bin 255 - i
+                for (int r = 0; r < cluster; ++r) c += of_rank(&hist[set][kBins - 1 - tid], r);
+                sum = c;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= o) sum += y;
+                }
+                if (lane == 31) s_warp[0][warp] = sum;
+            }
             __syncthreads();
-            need -= count(prefix + 1u, 0);
+            if (tid < kBins) {
+                const int before = sum - c + __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[0][lane] : 0);
+                if (before < need && need <= before + c) { s_pick[0] = kBins - 1 - tid; s_pick[1] = need - before; }
+            }
+            __syncthreads();
+            prefix |= (uint32_t)s_pick[0] << shift;
+            need = s_pick[1];
+            above = shift;
         }
     }
     // prefix: the threshold; need: how many of its equals stay, the lowest
@@ -394,12 +449,17 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
     equals = __reduce_add_sync(0xffffffffu, equals);
     __syncthreads();
     if (lane == 0) { s_warp[0][warp] = overs; s_warp[1][warp] = equals; }
-    if (tid == 0) s_gap = keep;
     __syncthreads();
+    if (warp == 0) {
+        overs = __reduce_add_sync(0xffffffffu, lane < kEWarps ? s_warp[0][lane] : 0);
+        equals = __reduce_add_sync(0xffffffffu, lane < kEWarps ? s_warp[1][lane] : 0);
+        if (lane == 0) { s_total[0] = overs; s_total[1] = equals; }
+    }
+    meet();
     // ---- the list: entry j goes to the number of overs below it and of the equals that stay.  The first gap is the first place
-    // whose entry comes from behind it.  (Each CTA writes the whole list, the same; it then reads its own.) ----
-    int at_over = __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[0][lane] : 0);
-    int at_equal = __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[1][lane] : 0);
+    // whose entry comes from behind it. ----
+    int at_over = __reduce_add_sync(0xffffffffu, (lane < warp ? s_warp[0][lane] : 0) + (lane < rank ? of_rank(&s_total[0], lane) : 0));
+    int at_equal = __reduce_add_sync(0xffffffffu, (lane < warp ? s_warp[1][lane] : 0) + (lane < rank ? of_rank(&s_total[1], lane) : 0));
     int gap = keep;
     each([&](int j, uint32_t x) {
         const bool o = over(j, x), e = equal(j, x);
@@ -414,8 +474,8 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
     });
     gap = __reduce_min_sync(0xffffffffu, gap);
     if (lane == 0 && gap < keep) atomicMin(&s_gap, gap);
-    __syncthreads();
-    gap = s_gap;
+    meet();                                       // (the list is there, too)
+    gap = __reduce_min_sync(0xffffffffu, lane < cluster ? of_rank(&s_gap, lane) : keep);
     const int wave = cluster * rows;
     // ---- the move ----
     constexpr int kPieces = kRowBytes / 16;
@@ -426,7 +486,7 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
     for (int r0 = gap; r0 < keep || r0 == gap; r0 += wave) {   // (once at least; every CTA of the cluster as often)
         const int to = r0 + rank * rows, count = max(0, min(rows, keep - to));
         for (int r = tid; r < count; r += kEThreads) {
-            const int src = list[to + r];
+            const int src = __ldcg(list + to + r);
             s_from[r] = src;
             s_w[r] = w[src];
         }
@@ -438,11 +498,7 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
             cp_async16(buffer + (rows * kPieces + i) * 16, vc + at);
         }
         cp_async_wait_all();
-        if (cluster > 1) {
-            asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-        } else {
-            __syncthreads();
-        }
+        meet();
         for (int r = tid; r < count; r += kEThreads) w[to + r] = s_w[r];
         for (int i = tid; i < count * kPieces; i += kEThreads) {
             const size_t at = (size_t)to * kRowBytes + i * 16;
@@ -462,7 +518,7 @@ cudaError_t launch_evict(void *k_cache, void *v_cache, float *weight, int32_t *c
     int cluster = 1;
     while (cluster < 8 && BH * cluster * 2 <= sm_count()) cluster *= 2;
     const int rows = (cluster > 1 ? 104 : 48) * 1024 / (2 * kRowBytes + 8), bytes = rows * (2 * kRowBytes + 8);
-    auto kernel = cap <= 2048 ? evict_kernel<kRowBytes, 4> : evict_kernel<kRowBytes, 16>;
+    auto kernel = cap <= 2048 * cluster ? evict_kernel<kRowBytes, 4> : evict_kernel<kRowBytes, 16>;
     cudaError_t e = allow_smem(kernel, 104 * 1024);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
