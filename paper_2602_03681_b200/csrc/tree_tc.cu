@@ -49,25 +49,35 @@ template <int D, int R> struct Layout {
     static constexpr int kRows = 16 * R;                     // nodes, padded
     using S = Sums<2, kRows>;
     using N = Nodes<2, kRows>;
-    // 16 warps per multiprocessor: two CTAs of 8, or one of 16.  Half of a CTA's warps read the cache, each 16 rows and a share of
-    // the tile's keys.
-    static constexpr int kCtas = R == 4 ? 1 : 2, kWarps = R == 4 ? 8 : 4, kHalf = 32 * kWarps, kThreads = 2 * kHalf;
-    static constexpr int kKeyGroups = kWarps / R, kWarpKeys = kTileKeys / kKeyGroups;
+    // Two CTAs of 8 warps per multiprocessor, or one of 16: half of a CTA's warps read the cache, each 16 rows and a share of the
+    // tile's keys.  Beyond 32 nodes of 128 columns the cache's products are tcgen05 MMAs: four warps of softmax and four that issue
+    // the copies of K and V and the two products, beside eight for the tree's own part.
+    static constexpr bool kUmma = R == 4 && D == 128;
+    static constexpr int kCtas = R == 4 ? 1 : 2, kWarps = R == 4 ? 8 : 4;      // kWarps: of the tree's part
+    static constexpr int kHalf = 32 * kWarps, kReaders = kUmma ? 256 : kHalf, kThreads = kReaders + kHalf;
+    static constexpr int kKeyGroups = kUmma ? 2 : kWarps / R, kWarpKeys = kTileKeys / kKeyGroups;
     static constexpr int kRowBytes = D * 2, kTileBytes = kTileKeys * kRowBytes;
-    static constexpr int kSlots = R == 4 ? (D == 128 ? 7 : 8) : D == 128 ? 4 : 6;
+    static constexpr int kSlots = kUmma ? 7 : R == 4 ? 8 : D == 128 ? 4 : 6;
     static constexpr int kAccPitch = D + 4;
     static constexpr int kCols = D / 2;                      // columns of a CTA, at most
     static constexpr int kPitch = kRowBytes + 16;            // (an odd number of 16-byte pieces: eight rows, eight banks)
     static constexpr int kPitchV = kCols * 2 + 16;
-    static constexpr int oQ = sizeof(S), oK = oQ + kRows * kPitch, oV = oK + kRows * kPitch, oTab = oV + kRows * kPitchV;
+    static constexpr int oK = sizeof(S), oV = oK + kRows * kPitch;
+    // q: padded rows, or an MMA operand: 64 columns after another, rows of 128 bytes, 16-byte pieces swizzled by row
+    static constexpr int oQ = (oV + kRows * kPitchV + (kUmma ? 1023 : 15)) / (kUmma ? 1024 : 16) * (kUmma ? 1024 : 16);
+    static constexpr int oTab = oQ + kRows * (kUmma ? kRowBytes : kPitch);
+    __host__ __device__ static constexpr int q_piece(int t, int c) {         // of piece c of row t, from oQ
+        return kUmma ? (c >> 3) * (kRows * 128) + t * 128 + (((c & 7) ^ (t & 7)) << 4) : t * kPitch + c * 16;
+    }
     // u and the linear read-out of the CTA's columns (the sums over the tree's V: over k); the probabilities over the tree, bf16
     static constexpr int oU = oTab + kRows * kRows * 4, oO = oU + kRows * kCols * 4, oP = oO + kRows * kCols * 4;
     static constexpr int kPitchP = kRows * 2 + 16;
     // the ring (16-byte pieces swizzled by row); at the end the key groups' results, the first one's place the CTA's
-    static constexpr int oRing = (oP + kRows * kPitchP + 127) / 128 * 128, kRing = kSlots * kTileBytes;
+    static constexpr int oRing = (oP + kRows * kPitchP + 1023) / 1024 * 1024, kRing = kSlots * kTileBytes;
     static constexpr int kMerge = kKeyGroups * kRows * kAccPitch * 4;
     static_assert(kMerge <= kRing, "the key groups' results lie in the ring");
     static constexpr int kTotal = oRing + kRing;
+    static_assert(!kUmma || kTotal + 8192 <= 232448, "an SM's shared memory, with the static part");
 };
 
 // The CTA's share of the cache: units 0, 1, 2, ... are K of tile 0, V of tile 0, K of tile 1, ...
@@ -104,14 +114,42 @@ template <int D, int R> struct Stream {
     }
 };
 
+// The key groups' results -> the CTA's.  group_m, group_z [G][key groups][rows]; acc [key groups][rows][pitch], the result in the
+// first one's place.
+template <int D, int G, int R>
+__device__ __forceinline__ void merge_groups(typename Layout<D, R>::S *sums, float *acc, const float *group_m, const float *group_z,
+                                             int n_nodes, int tid, int threads) {
+    using L = Layout<D, R>;
+    for (int i = tid; i < n_nodes * (D / 4); i += threads) {
+        const int t = i / (D / 4), x = (i - t * (D / 4)) * 4, s = x / (D / G);
+        float M = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < L::kKeyGroups; ++k) M = fmaxf(M, group_m[(s * L::kKeyGroups + k) * L::kRows + t]);
+        const float mu = M == -INFINITY ? 0.f : M;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        float Z = 0.f;
+#pragma unroll
+        for (int k = 0; k < L::kKeyGroups; ++k) {
+            const int at = (s * L::kKeyGroups + k) * L::kRows + t;
+            const float e = tc::ex2_ftz(group_m[at] - mu);
+            const float4 w = *reinterpret_cast<const float4 *>(acc + (k * L::kRows + t) * L::kAccPitch + x);
+            Z = fmaf(group_z[at], e, Z);
+            y.x = fmaf(w.x, e, y.x); y.y = fmaf(w.y, e, y.y);
+            y.z = fmaf(w.z, e, y.z); y.w = fmaf(w.w, e, y.w);
+        }
+        *reinterpret_cast<float4 *>(acc + t * L::kAccPitch + x) = y;
+        if (x % (D / G) == 0) { sums->cache_m[s][t] = M; sums->cache_z[s][t] = Z; }
+    }
+}
+
 template <int D, int G, bool kNorm, int R>
 __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t *sm, const Stream<D, R> &in, int n_nodes) {
     using L = Layout<D, R>;
     constexpr int ds = D / G, kNt = L::kWarpKeys / 8, kKs = ds / 16, kHalf = L::kHalf;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
     const int rg = warp / L::kKeyGroups, kg = warp - rg * L::kKeyGroups, r0 = rg * 16;
-    const uint32_t q_at = tc::smem_u32(sm + L::oQ) + (r0 + (lane & 15)) * L::kPitch + (lane >> 4) * 16;
-    auto load_q = [&](int k, uint32_t (&x)[4]) { ldmatrix_x4(q_at + k * 32, x); };
+    const uint32_t q_at = tc::smem_u32(sm + L::oQ) ;
+    auto load_q = [&](int k, uint32_t (&x)[4]) { ldmatrix_x4(q_at + L::q_piece(r0 + (lane & 15), 2 * k + (lane >> 4)), x); };
 
     // each row's factor to base-2 logits
     float f[2][kNorm ? G : 1];
@@ -286,25 +324,295 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
         }
     }
     tc::named_barrier_sync(1, kHalf);
-    for (int i = tid; i < n_nodes * (D / 4); i += kHalf) {
-        const int t = i / (D / 4), x = (i - t * (D / 4)) * 4, s = x / ds;
-        float M = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < L::kKeyGroups; ++k) M = fmaxf(M, s_m[s][k][t]);
-        const float mu = M == -INFINITY ? 0.f : M;
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        float Z = 0.f;
-#pragma unroll
-        for (int k = 0; k < L::kKeyGroups; ++k) {
-            const float e = tc::ex2_ftz(s_m[s][k][t] - mu);
-            const float4 w = *reinterpret_cast<const float4 *>(acc + (k * L::kRows + t) * L::kAccPitch + x);
-            Z = fmaf(s_z[s][k][t], e, Z);
-            y.x = fmaf(w.x, e, y.x); y.y = fmaf(w.y, e, y.y);
-            y.z = fmaf(w.z, e, y.z); y.w = fmaf(w.w, e, y.w);
-        }
-        *reinterpret_cast<float4 *>(acc + t * L::kAccPitch + x) = y;
-        if (x % ds == 0) { sums->cache_m[s][t] = M; sums->cache_z[s][t] = Z; }
+    merge_groups<D, G, R>(sums, acc, &s_m[0][0][0], &s_z[0][0][0], n_nodes, tid, kHalf);
+}
+
+// ------------------------------------------------------------------------------------------
+// The CTA's share of the cache with tcgen05 (33 to 64 nodes, 128 columns).  An MMA has 128 rows: the even tiles' logits use rows
+// 0 .. 63 of it, the odd ones' 64 .. 127 -- the operand is q behind, or ahead of, whatever shared memory holds there, and what the
+// other rows get is never looked at -- so that all four warps have a row per thread and tiles of their own, two key groups with a
+// running maximum each.  Probabilities take the logits' place in tensor memory as the second product's operand.  Per tile the
+// MMAs take 256 cycles; with warp-level MMAs a tile of 64 rows took 2900, twice the time that its bytes need.
+// ------------------------------------------------------------------------------------------
+struct UmmaBars {
+    uint64_t full[2][4], empty[2][4];             // [K, V][stage]
+    uint64_t s[4], p[4], o[4], drain[2];          // per place of logits: logits there, probabilities there, product done
+    uint32_t tmem;
+    int abort[2];
+};
+constexpr int kStagesK = 4, kStagesV = 3;         // (K is read twice where keys are normalised)
+__host__ __device__ constexpr int stages_of(int kv) { return kv ? kStagesV : kStagesK; }
+constexpr int kTmemCols = 512, kTmemO = 256;      // logits: four places of 64 columns; then the two groups' sums
+
+static_assert(kStagesK + kStagesV == Layout<128, 4>::kSlots, "");
+
+struct UmmaShare {
+    const CUtensorMap *map[2];
+    UmmaBars *bar;
+    uint8_t *sm, *ring;
+    int row, keys, tiles;                         // first row, keys, tiles of the share
+    __device__ int stage(int kv, int t) const { return kv ? t % kStagesV : t % kStagesK; }
+    __device__ uint32_t phase(int kv, int t) const { return (kv ? t / kStagesV : t / kStagesK) & 1; }
+    __device__ uint8_t *at(int kv, int t) const { return ring + (kv * kStagesK + stage(kv, t)) * (kTileKeys * 256); }
+};
+
+__device__ __forceinline__ void umma_init(UmmaBars *bar, bool norm, int wait_kcycles) {      // (one thread)
+    for (int s = 0; s < 4; ++s) {
+        for (int kv = 0; kv < 2; ++kv) { tc::mbar_init(&bar->full[kv][s], 1); tc::mbar_init(&bar->empty[kv][s], kv == 0 && norm ? 65 : 1); }
+        tc::mbar_init(&bar->s[s], 1);
+        tc::mbar_init(&bar->p[s], 64);
+        tc::mbar_init(&bar->o[s], 1);
     }
+    for (int i = 0; i < 2; ++i) tc::mbar_init(&bar->drain[i], 1);
+    bar->abort[0] = 0;
+    bar->abort[1] = wait_kcycles;
+    tc::fence_mbar_init();
+}
+// Places of a tile's logits: with one softmax head two per group, in turns; with two, one for each.
+template <int G> __device__ __forceinline__ int place_of(int t) { return (t & 1) * 2 + (G == 1 ? (t >> 1) & 1 : 0); }
+template <int G> __device__ __forceinline__ uint32_t place_phase(int t) { return (G == 1 ? t >> 2 : t >> 1) & 1; }
+
+// The issuing warps.  One that did all four took 2600 cycles a tile, half of them for issuing itself.
+// Copies of K (0) or V (1).
+__device__ void umma_load(const UmmaShare &in, int kv) {
+    using namespace tc;
+    UmmaBars *bar = in.bar;
+    const int tiles = (int)uniform((uint32_t)in.tiles), stages = stages_of(kv);
+    int t = 0;
+    for (; t < tiles; ++t) {
+        const int s = in.stage(kv, t);
+        if (t >= stages && !wait_all(&bar->empty[kv][s], in.phase(kv, t) ^ 1, bar->abort)) break;
+        if (elect_one()) {
+            mbar_arrive_expect_tx(&bar->full[kv][s], kTileKeys * 256);
+            for (int c = 0; c < 2; ++c) tma_load_2d(in.at(kv, t) + c * kTileKeys * 128, in.map[kv], &bar->full[kv][s], c * 64, in.row + t * kTileKeys);
+        }
+        __syncwarp();
+    }
+    if (t < tiles)                                // no copy in flight when the CTA retires
+        for (int i = max(0, t - stages); i < t; ++i) mbar_wait_drain(&bar->full[kv][in.stage(kv, i)], in.phase(kv, i));
+}
+
+__device__ __forceinline__ void umma_drain(uint64_t *bar) {              // no MMA in flight when the CTA retires
+    if (tc::elect_one()) {
+        tc::mma_commit(bar);
+        tc::mbar_wait_drain(bar, 0);
+    }
+    __syncwarp();
+}
+
+// Logits = q K^T into a tile's place, once the product that read the probabilities of the place's last tile is done.
+template <int G>
+__device__ void umma_logits(const UmmaShare &in, uint32_t tmem, uint32_t q_at) {
+    using namespace tc;
+    UmmaBars *bar = in.bar;
+    constexpr uint32_t idesc = make_idesc(kFmtBF16, 128, kTileKeys, false, false);
+    const int tiles = (int)uniform((uint32_t)in.tiles);
+    const uint32_t tm = uniform(tmem), aq = uniform(q_at);
+    bool ok = true;
+    for (int t = 0; ok && t < tiles; ++t) {
+        const int place = place_of<G>(t);
+        if (t >= (G == 1 ? 4 : 2)) ok = wait_all(&bar->o[place], place_phase<G>(t) ^ 1, bar->abort);
+        ok = ok && wait_all(&bar->full[0][in.stage(0, t)], in.phase(0, t), bar->abort);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t ak = uniform(smem_u32(in.at(0, t))), a0 = aq - (t & 1) * (64 * 128), ts = tm + 64 * place;
+        if (elect_one()) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    mma_ss(ts + (G == 2 ? 64 * c : 0), desc_kmajor(a0 + c * (64 * 128) + k * 32), desc_kmajor(ak + c * (kTileKeys * 128) + k * 32),
+                           idesc, G == 2 ? k != 0 : (c | k) != 0);
+            mma_commit(&bar->s[place]);
+            mma_commit(&bar->empty[0][in.stage(0, t)]);
+        }
+        __syncwarp();
+    }
+    if (!ok) umma_drain(&bar->drain[0]);
+}
+
+// The group's sums += probabilities V.
+template <int G>
+__device__ void umma_sums(const UmmaShare &in, uint32_t tmem) {
+    using namespace tc;
+    UmmaBars *bar = in.bar;
+    constexpr uint32_t idesc = make_idesc(kFmtBF16, 128, 128 / G, false, true);
+    const int tiles = (int)uniform((uint32_t)in.tiles);
+    const uint32_t tm = uniform(tmem);
+    bool ok = true;
+    for (int t = 0; ok && t < tiles; ++t) {
+        const int place = place_of<G>(t);
+        ok = wait_all(&bar->full[1][in.stage(1, t)], in.phase(1, t), bar->abort) && wait_all(&bar->p[place], place_phase<G>(t), bar->abort);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t av = uniform(smem_u32(in.at(1, t))), ts = tm + 64 * place, to = tm + kTmemO + 128 * (t & 1);
+        if (elect_one()) {
+#pragma unroll
+            for (int s = 0; s < G; ++s)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    mma_ts(to + 64 * s, ts + 64 * s + k * 8, desc_mnmajor(av + s * (kTileKeys * 128) + k * 2048, kTileKeys * 128), idesc,
+                           t > 1 || k != 0);
+            mma_commit(&bar->o[place]);
+            mma_commit(&bar->empty[1][in.stage(1, t)]);
+        }
+        __syncwarp();
+    }
+    if (!ok) umma_drain(&bar->drain[1]);
+}
+
+// The four softmax warps: thread = row of a key group.
+template <int G, bool kNorm>
+__device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, const UmmaShare &in, uint32_t tmem, int n_nodes) {
+    using namespace tc;
+    using L = Layout<128, 4>;
+    constexpr int ds = 128 / G;
+    __shared__ float s_m[G][2][64], s_z[G][2][64];
+    __shared__ __align__(16) float s_rk[kNorm ? 2 : 1][2][G][64];      // [group][in turns]: the keys' RMS factors
+    UmmaBars *bar = in.bar;
+    volatile int *abort_flag = bar->abort;
+    const int tid = threadIdx.x, warp = tid >> 5, g = warp >> 1, r = tid & 63;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kTmemO + 128 * g + lanes;
+    auto row_squares = [&](const uint8_t *tile, int row) {               // of 64 columns
+        float ss = 0.f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const uint4 y = *reinterpret_cast<const uint4 *>(tile + row * 128 + ((c ^ (row & 7)) << 4));
+            const float2 y0 = bf2(y.x), y1 = bf2(y.y), y2 = bf2(y.z), y3 = bf2(y.w);
+            ss += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
+        }
+        return ss;
+    };
+    float f[G], m[G], z[G];
+    {
+        float ss[2] = {0.f, 0.f};
+        if (kNorm)
+            for (int c = 0; c < 2; ++c) ss[c] = row_squares(in.sm + L::oQ + c * (64 * 128), r);
+#pragma unroll
+        for (int s = 0; s < G; ++s) {
+            f[s] = a.scale_sm * kLog2e;
+            if (kNorm) f[s] *= rsqrtf((G == 1 ? ss[0] + ss[1] : ss[s]) / ds + a.norm_eps);
+            m[s] = -INFINITY;
+            z[s] = 0.f;
+        }
+    }
+    bool ok = true;
+    int i = 0;                                    // the group's tiles so far
+    for (int t = g; t < in.tiles; t += 2, ++i) {
+        const int left = in.keys - t * kTileKeys;
+        ok = ok && wait_all(&bar->s[place_of<G>(t)], place_phase<G>(t), abort_flag);
+        if (kNorm) {                              // (the barrier below is everyone's, however the waits end)
+            ok = ok && wait_all(&bar->full[0][in.stage(0, t)], in.phase(0, t), abort_flag);
+            if (ok) {
+                const uint8_t *tile = in.at(0, t);
+                float ss[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) ss[c] = row_squares(tile + c * (kTileKeys * 128), r);
+#pragma unroll
+                for (int s = 0; s < G; ++s) s_rk[g][i & 1][s][r] = rsqrtf((G == 1 ? ss[0] + ss[1] : ss[s]) / ds + a.norm_eps);
+                mbar_arrive(&bar->empty[0][in.stage(0, t)]);
+            }
+            named_barrier_sync(3 + g, 64);
+        }
+        if (!ok) continue;
+        tc_fence_after_sync();
+#pragma unroll
+        for (int s = 0; s < G; ++s) {
+            const uint32_t ts = tmem + 64 * (place_of<G>(t) + s) + lanes;
+            float x[2][32];
+            float top = -INFINITY;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+                tmem_ld32(ts + 32 * hf, reinterpret_cast<uint32_t(&)[32]>(x[hf]));
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    float4 w = make_float4(1.f, 1.f, 1.f, 1.f);
+                    if (kNorm) w = *reinterpret_cast<const float4 *>(&s_rk[g][i & 1][s][32 * hf + c]);
+                    x[hf][c] *= f[s] * w.x; x[hf][c + 1] *= f[s] * w.y;
+                    x[hf][c + 2] *= f[s] * w.z; x[hf][c + 3] *= f[s] * w.w;
+                }
+                if (left < kTileKeys) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c)
+                        if (32 * hf + c >= left) x[hf][c] = -INFINITY;
+                }
+                float m4[4] = {x[hf][0], x[hf][1], x[hf][2], x[hf][3]};
+#pragma unroll
+                for (int c = 4; c < 28; c += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) m4[e] = max3(m4[e], x[hf][c + e], x[hf][c + 4 + e]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = max3(top, m4[e], x[hf][28 + e]);
+            }
+            const float m_old = m[s];
+            if (top > m_old + 8.f) m[s] = fmaxf(m_old, top);
+            const float mu = m[s] == -INFINITY ? 0.f : m[s], e = m[s] == m_old ? 1.f : ex2_ftz(m_old - mu);
+            uint32_t p[32];
+            float z2[2] = {0.f, 0.f};
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    const float p0 = ex2_ftz(x[hf][c] - mu), p1 = ex2_ftz(x[hf][c + 1] - mu);
+                    z2[hf] += p0 + p1;
+                    p[16 * hf + c / 2] = pack_bf162(p0, p1);
+                }
+            z[s] = fmaf(z[s], e, z2[0] + z2[1]);
+            tmem_st32(ts, p);
+            if (i > 0 && __any_sync(0xffffffffu, e != 1.f)) {
+                ok = wait_all(&bar->o[place_of<G>(t - 2)], place_phase<G>(t - 2), abort_flag);
+                if (ok) {
+                    tc_fence_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < ds; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(to + s * ds + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * e);
+                        tmem_st32(to + s * ds + c, o);
+                    }
+                }
+            }
+        }
+        tmem_wait_st();
+        if (left < kTileKeys && ok) {             // rows past the end count as zeros: what lies there may be anything
+            ok = wait_all(&bar->full[1][in.stage(1, t)], in.phase(1, t), abort_flag);
+            if (ok) {
+                uint8_t *tile = in.at(1, t);
+                for (int e = r; e < (kTileKeys - left) * 16; e += 64)
+                    *reinterpret_cast<uint4 *>(tile + (e & 1) * (kTileKeys * 128) + (left + (e >> 4)) * 128 + ((e >> 1) & 7) * 16) = make_uint4(0, 0, 0, 0);
+                fence_proxy_async_smem();
+            }
+        }
+        tc_fence_before_sync();
+        if (ok) mbar_arrive(&bar->p[place_of<G>(t)]);
+    }
+    const int t_last = g + 2 * (i - 1);           // (products are done in their order)
+    if (ok && i > 0) ok = wait_all(&bar->o[place_of<G>(t_last)], place_phase<G>(t_last), abort_flag);
+    tc_fence_after_sync();
+    named_barrier_sync(1, 128);                   // (both groups' tiles have been read: the ring is free)
+    float *acc = reinterpret_cast<float *>(in.ring), *mine = acc + (g * 64 + r) * L::kAccPitch;
+#pragma unroll 1
+    for (int c = 0; c < 128; c += 32) {
+        uint32_t o[32];
+        if (i > 0) {                              // (uniform)
+            tmem_ld32(to + c, o);
+            tmem_wait_ld();
+        } else {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = 0u;
+        }
+#pragma unroll
+        for (int y = 0; y < 32; y += 4) *reinterpret_cast<uint4 *>(mine + c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+    }
+    tc_fence_before_sync();
+    named_barrier_arrive(5, 192);                 // (an issuing warp gives tensor memory back)
+#pragma unroll
+    for (int s = 0; s < G; ++s) { s_m[s][g][r] = m[s]; s_z[s][g][r] = z[s]; }
+    named_barrier_sync(1, 128);
+    merge_groups<128, G, 4>(sums, acc, &s_m[0][0][0], &s_z[0][0][0], n_nodes, tid, 128);
 }
 
 // x as three bf16 terms, pairwise packed: what two rounded terms leave over is exact in the third.
@@ -334,7 +642,7 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                           int rank, bool odd, const NodeRow &node) {
     using L = Layout<D, R>;
     constexpr int ds = D / G, kRows = L::kRows, kNt = 2 * R, kKs = D / 16, kPieces = L::kRowBytes / 16, kHalf = L::kHalf, kWarps = L::kWarps;
-    const int tid = threadIdx.x - kHalf, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
+    const int tid = threadIdx.x - L::kReaders, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3, T = a.T;
     const int bh = b * a.H + h, cols = D / a.cluster, c0 = rank * cols, sc = c0 / ds;   // sc: the columns' softmax head
     auto sync = [] { tc::named_barrier_sync(2, kHalf); };
     float *tab = reinterpret_cast<float *>(sm + L::oTab);    // [j][i], i > j: what u_i takes from u_j
@@ -358,14 +666,13 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
     if (kNorm && tid < 2 * kRows) {               // a row's norms, thread = row of q or k
         const int t = tid % kRows;
         const bool is_k = tid >= kRows;
-        const uint8_t *row = sm + (is_k ? L::oK : L::oQ) + t * L::kPitch;
         float all = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             float ss = 0.f;
 #pragma unroll
             for (int c = g * kPieces / G; c < (g + 1) * kPieces / G; ++c) {
-                const uint4 y = *reinterpret_cast<const uint4 *>(row + c * 16);
+                const uint4 y = *reinterpret_cast<const uint4 *>(is_k ? sm + L::oK + t * L::kPitch + c * 16 : sm + L::oQ + L::q_piece(t, c));
                 const float2 y0 = bf2(y.x), y1 = bf2(y.y), y2 = bf2(y.z), y3 = bf2(y.w);
                 ss += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
             }
@@ -421,9 +728,9 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                 uint32_t ak[2][4], aq[2][4], bf[kPart][4];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const uint32_t off = (warp * 16 + (lane & 15)) * L::kPitch + (2 * (k + x) + (lane >> 4)) * 16;
-                    ldmatrix_x4(k_at + off, ak[x]);
-                    ldmatrix_x4(q_at + off, aq[x]);
+                    const int t = warp * 16 + (lane & 15), c = 2 * (k + x) + (lane >> 4);
+                    ldmatrix_x4(k_at + t * L::kPitch + c * 16, ak[x]);
+                    ldmatrix_x4(q_at + L::q_piece(t, c), aq[x]);
                 }
 #pragma unroll
                 for (int i = 0; i < kPart; ++i) ldmatrix_x4(k_at + ((i0 + i) * 8 + (lane & 7)) * L::kPitch + (2 * k + (lane >> 3)) * 16, bf[i]);
@@ -504,7 +811,10 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                     uint32_t af[kM][4];
 #pragma unroll
                     for (int m = 0; m < kM; ++m)
-                        ldmatrix_x4((m0 + m < R ? k_at : q_at) + ((m0 + m) % R * 16 + (lane & 15)) * L::kPitch + (2 * k + (lane >> 4)) * 16, af[m]);
+{
+                            const int t = (m0 + m) % R * 16 + (lane & 15), c = 2 * k + (lane >> 4);
+                            ldmatrix_x4(m0 + m < R ? k_at + t * L::kPitch + c * 16 : q_at + L::q_piece(t, c), af[m]);
+                        }
 #pragma unroll
                     for (int x = 2; x >= 0; --x)
 #pragma unroll
@@ -674,19 +984,26 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
 }
 
 template <int D, int G, bool kNorm, int R>
-__global__ void __launch_bounds__(Layout<D, R>::kThreads, Layout<D, R>::kCtas) tree_tc_kernel(Args a) {
+__global__ void __launch_bounds__(Layout<D, R>::kThreads, Layout<D, R>::kCtas)
+tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, Args a, int wait_kcycles) {
     using L = Layout<D, R>;
-    constexpr int kHalf = L::kHalf, kThreads = L::kThreads;
-    extern __shared__ __align__(128) uint8_t dyn_tc[];
+    constexpr int kReaders = L::kReaders, kThreads = L::kThreads;
+    extern __shared__ __align__(1024) uint8_t dyn_tc[];
     __shared__ typename L::N nodes;
+    __shared__ UmmaBars bars;
     const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, tid = threadIdx.x;
+    if (L::kUmma && tid == 128) {
+        umma_init(&bars, kNorm, wait_kcycles);
+        if (a.cap > 0) { tc::prefetch_tmap(&map_k); tc::prefetch_tmap(&map_v); }
+    }
     tc::grid_dependency_wait();
-    tc::launch_dependents();
-    const NodeRow node = load_node(a, b, h, tid >= kHalf ? tid - kHalf : a.T);
+    if (L::kUmma && tid / 32 == 4) tc::tmem_alloc(&bars.tmem, kTmemCols);
+    const NodeRow node = load_node(a, b, h, tid >= kReaders ? tid - kReaders : a.T);
     const int n = nodes_of(a, b), cols = D / a.cluster;
-    const Stream<D, R> in(a, dyn_tc, bh, tid, share_of(a.cache_len[bh], a.cap, a.cluster, rank));
+    const Share share = share_of(a.cache_len[bh], a.cap, a.cluster, rank);
+    const Stream<D, R> in(a, dyn_tc, bh, tid, share);
     typename L::S *sums = reinterpret_cast<typename L::S *>(dyn_tc);
-    if (tid < kHalf)
+    if (!L::kUmma && tid < kReaders)
 #pragma unroll
         for (int u = 0; u < L::kSlots - 1; ++u) in.fetch(u);
     // q, k and the columns of v
@@ -711,15 +1028,42 @@ __global__ void __launch_bounds__(Layout<D, R>::kThreads, Layout<D, R>::kCtas) t
     for (int i = 0; i < kLoads; ++i) {
         const int e = tid + i * kThreads, t = e / kPieces, c = e - t * kPieces;
         if (t < L::kRows) {
-            *reinterpret_cast<uint4 *>(dyn_tc + L::oQ + t * L::kPitch + c * 16) = x[0][i];
+            *reinterpret_cast<uint4 *>(dyn_tc + L::oQ + L::q_piece(t, c)) = x[0][i];
             *reinterpret_cast<uint4 *>(dyn_tc + L::oK + t * L::kPitch + c * 16) = x[1][i];
         }
     }
+    if (L::kUmma) {
+        tc::fence_proxy_async_smem();             // (q is an operand of the MMAs)
+        tc::tc_fence_before_sync();
+    }
     odd = __syncthreads_or(odd);
-    if (tid < kHalf) cache_part<D, G, kNorm, R>(a, sums, dyn_tc, in, n);
-    else tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank, odd, node);
+    tc::launch_dependents();
+    if (tid >= kReaders) {
+        tree_part<D, G, kNorm, R>(a, sums, dyn_tc, &nodes, b, h, n, rank, odd, node);
+    } else if constexpr (L::kUmma) {
+        tc::tc_fence_after_sync();
+        const uint32_t tmem = bars.tmem;
+        const int keys = share.to - share.from;
+        const UmmaShare u{{&map_k, &map_v}, &bars, dyn_tc, dyn_tc + L::oRing, bh * a.cap + share.from, keys, (keys + kTileKeys - 1) / kTileKeys};
+        if (tid < 128) {
+            umma_softmax<G, kNorm>(a, sums, u, tmem, n);
+        } else if (tid < 160) {
+            umma_sums<G>(u, tmem);
+            tc::named_barrier_sync(5, 192);
+            tc::tc_fence_after_sync();
+            tc::tmem_dealloc(tmem, kTmemCols);
+        } else if (tid < 192) {
+            umma_logits<G>(u, tmem, tc::smem_u32(dyn_tc + L::oQ));
+            tc::named_barrier_arrive(5, 192);
+        } else {
+            umma_load(u, (tid >> 5) & 1);
+        }
+    } else {
+        cache_part<D, G, kNorm, R>(a, sums, dyn_tc, in, n);
+    }
     join_rows<__nv_bfloat16, D>(a, b, h, n, rank, sums, reinterpret_cast<const float *>(dyn_tc + L::oRing), L::kAccPitch,
                                 reinterpret_cast<const float *>(dyn_tc + L::oO), reinterpret_cast<const float *>(dyn_tc + L::oK));
+    if (L::kUmma && tid == 0 && bars.abort[0]) atomicMin(a.status, (int)NATSL_ERR_TIMEOUT);
 }
 
 template <int D, int G, bool kNorm, int R>
@@ -727,7 +1071,12 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     auto kernel = tree_tc_kernel<D, G, kNorm, R>;
     cudaError_t e = allow_smem(kernel, Layout<D, R>::kTotal);
     if (e != cudaSuccess) return e;
-    return launch_clusters(kernel, BH * a.cluster, a.cluster, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st, a);
+    CUtensorMap map_k = {}, map_v = {};
+    if (Layout<D, R>::kUmma && a.cap > 0 && (!tch::make_map_2d(&map_k, a.k_cache, (uint64_t)BH * a.cap, D, kTileKeys) ||
+                                             !tch::make_map_2d(&map_v, a.v_cache, (uint64_t)BH * a.cap, D, kTileKeys)))
+        return cudaErrorInvalidValue;
+    return launch_clusters(kernel, BH * a.cluster, a.cluster, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st, map_k, map_v, a,
+                           debug_wait_kcycles());
 }
 template <int D, int G, bool kNorm>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
