@@ -155,10 +155,6 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
     constexpr int V = D / 32, cols = D / kCluster;
     const int lane = threadIdx.x & 31, G = a.G, ls = 32 / G, sg = lane / ls, step = kCluster * (blockDim.x >> 5);
     const int owner = lane * V / cols, at = lane * V - owner * cols;
-    // the rows' weights, a lane each, on their way before the barrier (a warp has 32 rows at most)
-    const int t_first = rank + kCluster * (threadIdx.x >> 5), t_lane = t_first + lane * step;
-    float2 w = make_float2(0.5f, 0.5f);
-    if (a.w && t_lane < n) w = *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t_lane) * a.H + h) * 2);
     struct Row {
         float m[kCluster], z[kCluster], x[kCluster][V], mt, zt, o[V], la[V];
     };
@@ -200,9 +196,8 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
         if (last) cluster_arrive();               // (the warp has read its last row)
         for (int s = ls / 2; s > 0; s >>= 1) sn += __shfl_xor_sync(0xffffffffu, sn, s);
         sl = warp_sum(sl);
-        const int i_row = (t - t_first) / step;
-        const float wn = __shfl_sync(0xffffffffu, w.x, i_row), wl = __shfl_sync(0xffffffffu, w.y, i_row);
-        const float fn = wn * rsqrtf(sn / (D / G) + a.eps), fl = wl * rsqrtf(sl / D + a.eps);
+        const float2 w = a.w ? *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t) * a.H + h) * 2) : make_float2(0.5f, 0.5f);
+        const float fn = w.x * rsqrtf(sn / (D / G) + a.eps), fl = w.y * rsqrtf(sl / D + a.eps);
         ST *out = reinterpret_cast<ST *>(a.out) + (((size_t)b * a.T + t) * a.H + h) * D + lane * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) y.o[i] = fmaf(fn, y.o[i], fl * y.la[i]);
@@ -215,7 +210,7 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
         if (a.lse && lane % ls == 0)
             a.lse[(((size_t)b * a.H + h) * G + sg) * a.T + t] = Z == 0.f ? -INFINITY : (M + log2f(Z)) * kLn2;
     };
-    int t = t_first;
+    int t = rank + kCluster * (threadIdx.x >> 5);
     Row y;
     cluster_arrive();
     cluster_wait();
