@@ -544,6 +544,7 @@ cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t 
                                  const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg,
                                  bool tensor_cores, cudaStream_t st) {
     if (tensor_cores && hg.G <= 2) {
+        if (s.d == 128 && s.L > 32) return launch_weights_umma(q, lse, visible, k_cache, cache_len, cap, weight, scale, s, hg, st);
 #define ARGS q, lse, visible, k_cache, cache_len, cap, weight, scale, s, hg.norm_eps, st
 #define BY_ROWS(D, G, N)                                                                                                   \
     return s.L <= 16 ? launch_weights_tc<D, G, N, 1>(ARGS) : s.L <= 32 ? launch_weights_tc<D, G, N, 2>(ARGS) : launch_weights_tc<D, G, N, 4>(ARGS)
