@@ -196,8 +196,8 @@ __device__ __forceinline__ void join_rows_of(const Args &a, int b, int h, int n,
         if (last) cluster_arrive();               // (the warp has read its last row)
         for (int s = ls / 2; s > 0; s >>= 1) sn += __shfl_xor_sync(0xffffffffu, sn, s);
         sl = warp_sum(sl);
-        const float2 w = a.w ? *reinterpret_cast<const float2 *>(a.w + (((size_t)b * a.T + t) * a.H + h) * 2) : make_float2(0.5f, 0.5f);
-        const float fn = w.x * rsqrtf(sn / (D / G) + a.eps), fl = w.y * rsqrtf(sl / D + a.eps);
+        const float *w = a.w + (((size_t)b * a.T + t) * a.H + h) * 2;
+        const float fn = (a.w ? w[0] : 0.5f) * rsqrtf(sn / (D / G) + a.eps), fl = (a.w ? w[1] : 0.5f) * rsqrtf(sl / D + a.eps);
         ST *out = reinterpret_cast<ST *>(a.out) + (((size_t)b * a.T + t) * a.H + h) * D + lane * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) y.o[i] = fmaf(fn, y.o[i], fl * y.la[i]);

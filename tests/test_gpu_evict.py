@@ -79,20 +79,36 @@ def test_weights(dtype, d, G, norm, flags, T):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("T", [5, 30])
+@pytest.mark.parametrize("T", [5, 30, 40])
 def test_weights_of_every_length(dtype, T):
     x = case(3, 3, 5, T, 128, LENGTHS, 600, dtype)
     weigh(x, dtype)
     weigh(x, dtype, visible=False)
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_rows_that_count_for_nothing(dtype):
+@pytest.mark.parametrize("G,norm", [(1, False), (1, True), (2, False), (2, True)])
+@pytest.mark.parametrize("T", [33, 65, 128, 200])
+def test_weights_of_many_rows(G, norm, T):
+    """Rows by the 64, keys by the 128, runs of 256 and more of them."""
+    x = case(T, 2, 2, T, 128, [1200, 0, 129, 256, 640], 1200, "bf16", G, norm)
+    weigh(x, "bf16", G, norm)
+    weigh(x, "bf16", G, norm, visible=False)
+
+
+def test_weights_of_many_pairs():
+    """Runs of more than the shortest length."""
+    x = case(5, 8, 16, 40, 128, [1500, 31, 800, 1024, 1025], 1500, "bf16")
+    weigh(x, "bf16")
+
+
+@pytest.mark.parametrize("dtype,T", [("f32", 9), ("bf16", 9), ("bf16", 70)])
+def test_rows_that_count_for_nothing(dtype, T):
     """A row whose log-sum-exp is not finite, whatever its query holds; entries behind the length, whatever they hold; an
     entry that is NaN gets a NaN of its own."""
-    x = case(4, 1, 2, 9, 64, [50, 17], 60, dtype)
+    d = 64 if T < 32 else 128
+    x = case(4, 1, 2, T, d, [50, 17], 60, dtype)
     x["visible"][:] = 60
-    x["lse"] = logits(x, 8.0, 1, False)
+    x["lse"] = logits(x, d ** 0.5, 1, False)
     x["lse"][:, :, :, 2], x["lse"][:, :, :, 3], x["lse"][:, :, :, 4] = -np.inf, np.inf, np.nan
     x["q"][:, 2:5] = np.nan
     x["k_cache"][0, 0, 50:], x["k_cache"][0, 1, 17:] = np.nan, np.inf

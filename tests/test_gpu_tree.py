@@ -121,6 +121,33 @@ def test_long_cache(dtype):
     check(call(x, dtype), reference(x), dtype)
 
 
+@pytest.mark.parametrize("G,norm", [(1, False), (1, True), (2, False), (2, True)])
+@pytest.mark.parametrize("T,cluster", [(33, 8), (64, 4), (49, 2)])
+def test_full_trees_over_long_caches(G, norm, T, cluster):
+    """33 to 64 nodes: several turns of the ring, every number of tiles modulo its places, one to eight CTAs' shares."""
+    B, H = {8: (1, 9), 4: (3, 10), 2: (6, 10)}[cluster]
+    lengths = [1800, 0, 1, 63, 64, 65, 640, 704, 768, 832, 896, 960, 1024, 1088, 1151, 1153, 1799, 17, 700]
+    x = make(T + G, B, H, T, 128, lengths, 1800, "bf16", route="all", unit=not norm)
+    check(call(x, "bf16", G=G, norm=norm), reference(x, G, norm), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weights_of_the_branches_at_any_address(dtype):
+    """p->w is an fp32 array like the others: nothing but its elements' alignment is asked for."""
+    from paper_2602_03681_b200 import binding
+    x = make(12, 2, 3, 9, 64, [0, 30, 77], 80, dtype)
+    t = call(x, dtype)
+    first = t["out"].clone()
+    shifted = torch.empty(t["w"].numel() + 1, device="cuda")[1:].view_as(t["w"])
+    shifted.copy_(t["w"])
+    B, T, H, d = x["q"].shape
+    la, sm = scales(d, 1, False)
+    t["p"] = binding.make_params(B, H, T, d, binding._dtype_code(t["q"]), la, sm, w=shifted, lse=t["lse"])
+    t["out"].fill_(SENTINEL)
+    step(t)
+    assert torch.equal(t["out"], first)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("nodes", [[0, 5], [13, 1, 7], [0, 0]])
 def test_ragged_trees(dtype, nodes):
@@ -178,10 +205,11 @@ def test_nothing_visible_and_optional_arguments(dtype):
     check(call(x, dtype, w=False, want_u=False, want_lse=False), reference(x, w=False), dtype)
 
 
-def test_large_logits():
+@pytest.mark.parametrize("T", [6, 50])
+def test_large_logits(T):
     """Logits of several hundred: the running maximum keeps exponentials in range."""
     for dtype in ("f32", "bf16"):
-        x = make(9, 1, 2, 6, 128, [200, 77], 200, dtype)
+        x = make(9, 1, 2, T, 128, [200, 77], 200, dtype)
         x["q"] *= 32
         ref = reference(x)
         t = call(x, dtype, want_lse=False)
@@ -209,9 +237,25 @@ def test_what_is_not_a_tree_is_reported(dtype):
     check(call(x, dtype), ref, dtype)
 
 
-@pytest.mark.parametrize("dtype,G,norm", [("f32", 1, False), ("bf16", 1, False), ("bf16", 2, True)])
-def test_results_do_not_depend_on_who_finishes_last(dtype, G, norm):
-    x = make(11, 4, 8, 24, 128, LENGTHS, 600, dtype, unit=not norm)
+def test_logits_that_grow_along_the_cache():
+    """Every tile raises the running maximum by more than the sums' slack, so that all sums are rescaled again and again."""
+    for T, G in ((9, 1), (40, 1), (40, 2)):
+        x = make(T, 1, 2, T, 128, [900, 641], 900, "bf16", unit=True)
+        # keys along the first nodes' mean direction, longer from tile to tile: logits grow to about 100
+        x["q"][:] = x["q"][:, :1]
+        ramp = np.linspace(0.0, 8.0, 900)[:, None]
+        x["k_cache"] = (ramp * x["q"][:, 0][:, :, None, :]).astype(np.float32)
+        x["k_cache"] = torch.from_numpy(x["k_cache"]).bfloat16().float().numpy().astype(x["v_cache"].dtype)
+        ref = reference(x, G)
+        t = call(x, "bf16", G=G, want_lse=False)
+        # (a logit of 91 carries up to 91 * 128 * 2^-24 = 7e-4, and so does the probability it gives)
+        check_stored(t["out"].float().cpu().numpy(), ref["out"], TOL["bf16"], "bf16")
+
+
+@pytest.mark.parametrize("dtype,G,norm,T", [("f32", 1, False, 24), ("bf16", 1, False, 24), ("bf16", 2, True, 24), ("bf16", 1, False, 64),
+                                            ("bf16", 2, True, 64)])
+def test_results_do_not_depend_on_who_finishes_last(dtype, G, norm, T):
+    x = make(11, 4, 8, T, 128, LENGTHS, 600, dtype, unit=not norm)
     t = call(x, dtype, G=G, norm=norm)
     first = [t[m].clone() for m in ("out", "u", "lse")]
     for _ in range(20):
@@ -296,11 +340,11 @@ def test_step_and_commit_are_generation(dtype, G, norm):
         assert rel_err(t["state"][b].cpu().numpy(), one["state"][0].cpu().numpy()) <= 1e-4
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_captured_and_on_another_stream(dtype):
+@pytest.mark.parametrize("dtype,T", [("f32", 10), ("bf16", 10), ("bf16", 45)])
+def test_captured_and_on_another_stream(dtype, T):
     """Step and commit in a CUDA graph, replayed on new contents; two graphs that share a workspace, one after the other; a
     stream that is not the default one."""
-    x = make(31, 2, 4, 10, 128, [5, 70, 200, 0], 260, dtype, route="all")
+    x = make(31, 2, 4, T, 128, [5, 70, 200, 0], 260, dtype, route="all")
     t = call(x, dtype)
     eager = [t[m].clone() for m in ("out", "u", "lse")]
     start = [t[m].clone() for m in ("state", "k_cache", "v_cache", "cache_len")]
@@ -333,3 +377,52 @@ def test_captured_and_on_another_stream(dtype):
     side.synchronize()
     assert all(torch.equal(t[m], e) for m, e in zip(("out", "u", "lse"), eager))
     check_commit(t, x)
+
+
+def test_beside_other_users_of_tensor_memory():
+    """Full trees, cache weights and the prompt's forward, on three streams at once, each with a workspace of its own."""
+    from paper_2602_03681_b200 import binding
+    x = make(41, 4, 8, 64, 128, [600, 5, 333, 64], 700, "bf16")
+    t = call(x, "bf16")
+    B, T, H, d = x["q"].shape
+    la, sm = scales(d, 1, False)
+    weight = torch.zeros(B, H, 700, device="cuda")
+    pw = binding.make_params(B, H, T, d, binding._dtype_code(t["q"]), la, sm)
+    L = 512
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn(1, L, 4, d, device="cuda", generator=gen) for _ in range(3))
+    q, k, v = (torch.nn.functional.normalize(y, dim=-1).bfloat16() for y in (q, k, v))
+    g, beta = -torch.rand(1, L, 4, device="cuda", generator=gen), torch.rand(1, L, 4, device="cuda", generator=gen)
+    route = (torch.rand(1, L, 4, device="cuda", generator=gen) < 0.3).to(torch.uint8)
+    out = torch.empty_like(q)
+    pf = binding.make_params(1, 4, L, d, binding._dtype_code(q), la, sm)
+    wf = binding.alloc_workspace(pf, binding.OP_FWD)
+
+    def weights():
+        binding.natsl_cache_weights(t["q"], t["lse"], None, t["k_cache"], t["cache_len"], weight, pw)
+
+    def forward():
+        binding.natsl_hybrid_fwd(q, k, v, g, beta, route, out, pf, wf)
+
+    want = [t[m].clone() for m in ("out", "u")]
+    weights()
+    forward()
+    torch.cuda.synchronize()
+    once, fwd = weight.clone(), out.clone()
+    weight.zero_()
+    lse = t["lse"].clone()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        with torch.cuda.stream(streams[0]):
+            step(t)
+        with torch.cuda.stream(streams[1]):
+            weight.zero_()
+            binding.natsl_cache_weights(t["q"], lse, None, t["k_cache"], t["cache_len"], weight, pw)
+        with torch.cuda.stream(streams[2]):
+            forward()
+    torch.cuda.synchronize()
+    assert all(torch.equal(t[m], y) for m, y in zip(("out", "u"), want))
+    assert torch.equal(weight, once) and torch.equal(out, fwd)
+    assert binding.natsl_device_status(t["ws"]) == 0 and binding.natsl_device_status(wf) == 0
