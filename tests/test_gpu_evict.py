@@ -279,3 +279,39 @@ def test_generation_with_a_bounded_cache(dtype, G, norm):
         visible = (n_before[:, None] + kept.cumsum(1)).to(torch.int32)
         weigh_and_evict(q, rows, visible, weight)
         assert binding.natsl_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 40), ("f32", 9)])
+def test_offsets_past_32_bits(dtype, T):
+    """Caches of more than 2^31 elements a pair: the second pair's lies behind them.  All four calls give what they give for
+    the same entries in a small cache."""
+    from paper_2602_03681_b200 import binding
+    d, cap, big, keep = 128, 400, 2 ** 24 + 64, 100
+    if torch.cuda.mem_get_info()[0] < 6 * big * d * (2 if dtype == "bf16" else 4):
+        pytest.skip("not enough device memory")
+    x = make(6, 1, 2, T, d, [300, 290], cap, dtype)
+    t = {n: dev(x[n], torch.bfloat16 if dtype == "bf16" and n in ("q", "k", "v", "k_cache", "v_cache") else None) for n in x
+         if x[n] is not None}
+    la, sm = scales(d, 1, False)
+    results = []
+    for rows in (cap, big):
+        kc = torch.empty(1, 2, rows, d, dtype=t["k_cache"].dtype, device="cuda")
+        vc, weight = torch.empty_like(kc), torch.zeros(1, 2, rows, device="cuda")
+        kc[:, :, :cap], vc[:, :, :cap] = t["k_cache"], t["v_cache"]
+        out, u = torch.empty_like(t["q"]), torch.empty(1, T, 2, d, device="cuda")
+        lse, state, length = torch.empty(1, 2, T, device="cuda"), t["state"].clone(), t["cache_len"].clone()
+        kept = torch.full((1, 2, keep), -1, dtype=torch.int32, device="cuda")
+        p = binding.make_params(1, 2, T, d, binding._dtype_code(out), la, sm, w=t["w"], lse=lse)
+        ws = binding.alloc_workspace(p, binding.OP_TREE)
+        binding.natsl_tree_step(t["q"], t["k"], t["v"], t["g"], t["beta"], t["route"], t["parent"], None, state, kc, vc, length, out, u,
+                                p, ws)
+        binding.natsl_tree_commit(t["k"], t["v"], t["g"], t["route"], u, t["path"], t["n_path"], state, kc, vc, length, p, ws)
+        binding.natsl_cache_weights(t["q"], lse, None, kc, length, weight, p)
+        grown = [kc[:, :, :cap].clone(), vc[:, :, :cap].clone(), length.clone()]
+        binding.natsl_cache_evict(kc, vc, weight, length, keep, 2, 10, kept, p)
+        assert binding.natsl_device_status(ws) == 0
+        results.append([out, u, lse, state, length, kept, weight[:, :, :keep].clone(), kc[:, :, :keep].clone(), vc[:, :, :keep].clone()] +
+                       [g[:, h, :grown[2][0, h]] if g.dim() > 2 else g for g in grown for h in range(2)])
+        del kc, vc, weight
+        torch.cuda.empty_cache()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
