@@ -360,8 +360,9 @@ int natsl_decode_block_end(const uint8_t *route_block, const float *g_block, flo
  * p->G in {1, 2, 4} with d / G >= 32 and NATSL_QK_NORM as in natsl_decode_step.  bf16 storage runs on the
  * tensor cores, except with NATSL_FORCE_SIMT or four softmax heads.  A parent that is not below its node
  * counts as -1 and is reported as NATSL_ERR_TREE, like a count outside [0, L] (the nearer of both).
- * ws holds natsl_workspace_size(p, NATSL_OP_TREE) bytes, is zero-filled once before its first use and is not
- * shared by calls that overlap on the GPU.  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, UNSUPPORTED, CUDA.
+ * ws holds natsl_workspace_size(p, NATSL_OP_TREE) bytes (the status word of natsl_device_status alone, TIMEOUT
+ * among its values), is zero-filled once before its first use and is not shared by calls that overlap on the
+ * GPU.  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, UNSUPPORTED, CUDA.
  */
 int natsl_tree_step(const void *q, const void *k, const void *v, const float *g, const float *beta,
                     const uint8_t *route, const int32_t *parent, const int32_t *n_nodes, const float *state,
@@ -397,8 +398,8 @@ int natsl_tree_commit(const void *k, const void *v, const float *g, const uint8_
  *       running sum of `route` over L), or NULL for all of them;
  *   k_cache [B,H,cache_cap,d], cache_len [B,H]: read (a length outside [0, cache_cap] counts as the nearer of
  *       both); weight [B,H,cache_cap] fp32: updated in place, entries from the length on are left alone.
- * NATSL_QK_NORM and p->G as in natsl_tree_step.  No workspace.  Errors: NULL, SHAPE, DTYPE, ALIGN,
- * UNSUPPORTED, CUDA.
+ * NATSL_QK_NORM and p->G as in natsl_tree_step.  No workspace, and so no status word: should a wait inside the
+ * kernel run out, entries get a NaN.  Errors: NULL, SHAPE, DTYPE, ALIGN, UNSUPPORTED, CUDA.
  */
 int natsl_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
                         const int32_t *cache_len, int32_t cache_cap, float *weight, const natsl_params *p,

@@ -6,7 +6,8 @@
 // Bound by memory up to some 64 exponentials a key, then by those: a multiprocessor takes 11 cycles to get a key's 256 bytes and
 // one for 16 exponentials.  Two CTAs per multiprocessor, each with 64 rows of q at a time as the B operand and a ring of five half
 // tiles of K (128 keys, 64 columns: with two softmax heads, a head's).  Two groups of four warps take tiles in turns; one warp
-// issues copies, one MMAs.
+// issues copies, one MMAs.  B200: 64 rows, two heads, 4 x 16 caches of up to 3277 keys 22.6 us, where warp-level MMAs took
+// 26.7: of a CTA's 24000 cycles 12300 are the exponentials of its multiprocessor, 4000 the start up to the rows' factors.
 #include <algorithm>
 #include "common.cuh"
 #include "natsl_internal.h"

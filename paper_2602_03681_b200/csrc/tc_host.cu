@@ -60,7 +60,7 @@ bool make_map_blhd(CUtensorMap *m, const void *base, int B, int L, int H, int d,
 
 cudaError_t allow_smem_of(const void *kernel, int bytes, bool all_shared) {
     struct Entry { const void *fn; int dev; };
-    constexpr int kEntries = 128;                     // (the library has fewer kernels; a full table only re-sends)
+    constexpr int kEntries = 256;                     // (the library has fewer kernels; a full table only re-sends)
     thread_local Entry table[kEntries] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

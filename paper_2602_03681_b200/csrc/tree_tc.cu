@@ -1,19 +1,25 @@
 // Tree step on the tensor cores (bf16 storage): the hybrid layer over a tree of up to 64 drafted tokens.  The mathematics is
-// tree_simt.cu's; here the products are warp-level MMAs: a tree has 1 to 64 query rows, far below a tcgen05 tile of 128, and
-// the call is bound by reading the retained K/V once.
+// tree_simt.cu's.
 //
-// A CTA has two halves that work side by side and meet at the end.  Half of the warps read the CTA's share of the cache: tiles of 64
-// keys through a ring of asynchronous copies, K and V in turns.  They share the tile by keys (and, beyond 16 nodes, by two
-// groups of 16), each with its own running maximum and sum, so that a key's row leaves shared memory once (twice)
-// whatever the number of nodes; the warps' results meet at the end.  A running maximum moves only when a logit exceeds it by
-// 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's own precision); their sum is taken before the rounding.
+// A CTA has two parts that work side by side and meet at the end.  Some warps read the CTA's share of the cache, in tiles of 64
+// keys.  Up to 32 nodes (and with 64 columns) they are half of the warps and use warp-level MMAs: a tree has few query rows
+// for a tcgen05 tile of 128, and the call is bound by reading K/V once.  K and V pass in turns through a ring of asynchronous
+// copies; the warps share the tile by keys (and, beyond 16 nodes, by two groups of 16), each with its own running maximum and
+// sum, so that a key's row leaves shared memory once (twice) whatever the number of nodes, and their results meet at the
+// end.  Beyond 32 nodes of 128 columns that arithmetic takes twice the time of the bytes, and tcgen05 takes it over (below).
+// A running maximum moves only when a logit exceeds it by 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's
+// own precision); their sum is taken before the rounding.
 //
-// The other warps compute the tree's own part, for the CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32 state as three bf16 terms that
-// together hold all of its 24 bits, so that u, which goes into the state at the commit, is as exact as on CUDA cores; the
-// substitution for u in fp32, a thread per column, by blocks of 16 nodes without a look at the tree's shape (the table is
-// zero off the path); the read-outs as MMAs again, u and the table as two bf16 terms each (2^-16).  Zeros in the place of
-// what a node does not see would let an infinity or a NaN through, so values that are not finite take a slower way that
-// looks at the paths.
+// The other warps compute the tree's own part, for the CTA's columns: the T x T tables as MMAs; k S0 and q S0 with the fp32
+// state as three bf16 terms that together hold all of its 24 bits, so that u, which goes into the state at the commit, is as
+// exact as on CUDA cores; the substitution for u in fp32, a thread per column, by blocks of 16 nodes without a look at the
+// tree's shape (the table is zero off the path); the read-outs as MMAs again, u and the table as two bf16 terms each (2^-16).
+// Zeros in the place of what a node does not see would let an infinity or a NaN through, so values that are not finite take
+// a slower way that looks at the paths.
+//
+// B200: one token of 64 x 16 heads over 1638 keys 155 us (930 MB: 6.0 TB/s, 92 % of a copy's rate); 32 nodes 216 us (4.5 TB/s:
+// of a CTA's 53000 cycles the last 10000 are the join, which no load overlaps but the neighbour CTA's); 64 nodes of 8 x 16
+// heads over up to 6554 keys 92 us (161 us with warp-level MMAs); 16 nodes of 16 heads 11 us.
 #include <algorithm>
 #include "tree_common.cuh"
 
@@ -51,7 +57,8 @@ template <int D, int R> struct Layout {
     using N = Nodes<2, kRows>;
     // Two CTAs of 8 warps per multiprocessor, or one of 16: half of a CTA's warps read the cache, each 16 rows and a share of the
     // tile's keys.  Beyond 32 nodes of 128 columns the cache's products are tcgen05 MMAs: four warps of softmax and four that issue
-    // the copies of K and V and the two products, beside eight for the tree's own part.
+    // the copies of K and V and the two products, beside eight for the tree's own part.  (The same for 17 to 32 nodes, with one
+    // softmax warp a CTA: 224 us where warp-level MMAs take 216.)
     static constexpr bool kUmma = R == 4 && D == 128;
     static constexpr int kCtas = R == 4 ? 1 : 2, kWarps = R == 4 ? 8 : 4;      // kWarps: of the tree's part
     static constexpr int kHalf = 32 * kWarps, kReaders = kUmma ? 256 : kHalf, kThreads = kReaders + kHalf;
@@ -372,7 +379,7 @@ __device__ __forceinline__ void umma_init(UmmaBars *bar, bool norm, int wait_kcy
 template <int G> __device__ __forceinline__ int place_of(int t) { return (t & 1) * 2 + (G == 1 ? (t >> 1) & 1 : 0); }
 template <int G> __device__ __forceinline__ uint32_t place_phase(int t) { return (G == 1 ? t >> 2 : t >> 1) & 1; }
 
-// The issuing warps.  One that did all four took 2600 cycles a tile, half of them for issuing itself.
+// The issuing warps.  One that did all four took 2600 cycles a tile, half of them for issuing itself: 145 us where four take 92.
 // Copies of K (0) or V (1).
 __device__ void umma_load(const UmmaShare &in, int kv) {
     using namespace tc;
