@@ -131,6 +131,8 @@ cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__
     __shared__ __align__(8) float s_key[kNorm ? G : 1][kTTile];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
     const int rg = warp / kKeyGroups, kg = warp - rg * kKeyGroups, r0 = rg * 16 * kMt;
+    tc::grid_dependency_wait();
+    tc::launch_dependents();
     const int bh = blockIdx.x / runs, b = bh / H, h = bh - b * H, n = min(max(cache_len[bh], 0), cap);
     const int from = (blockIdx.x - bh * runs) * run, to = min(n, from + run), tiles = (to - from + kTTile - 1) / kTTile;
     if (from >= n) return;
@@ -327,10 +329,10 @@ cudaError_t launch_weights_tc(const void *q, const float *lse, const int32_t *vi
     auto kernel = cache_weights_tc_kernel<D, G, kNorm, R>;
     cudaError_t e = allow_smem(kernel, ring + 2 * kMaxRun * 4);
     if (e != cudaSuccess) return e;
-    kernel<<<(int)BH * runs, kWThreads, ring + (R > 2 ? 2 : 1) * run * 4, st>>>(
-        (const uint8_t *)q, lse, visible, (const uint8_t *)k_cache, cache_len, cap, weight, s.H, s.L, scale, norm_eps, runs, run);
+    e = launch_kernel(kernel, dim3((unsigned)(BH * runs)), dim3(kWThreads), ring + (R > 2 ? 2 : 1) * run * 4, st, true, (const uint8_t *)q,
+                      lse, visible, (const uint8_t *)k_cache, cache_len, cap, weight, s.H, s.L, scale, norm_eps, runs, run);
     count_launch();
-    return cudaGetLastError();
+    return e;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -358,6 +360,8 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
     __shared__ int hist[2][kBins], s_warp[2][kEWarps], s_pick[2], s_total[2], s_gap;
     __shared__ uint32_t s_all, s_any;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bh = blockIdx.x / cluster, rank = blockIdx.x - bh * cluster;
+    tc::grid_dependency_wait();
+    tc::launch_dependents();
     float *w = weight + (size_t)bh * cap;
     int32_t *list = kept + (size_t)bh * keep;
     const int n = min(max(cache_len[bh], 0), cap);
@@ -531,12 +535,14 @@ cudaError_t launch_evict(void *k_cache, void *v_cache, float *weight, int32_t *c
     cfg.blockDim = dim3(kEThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, kernel, (uint8_t *)k_cache, (uint8_t *)v_cache, weight, cache_len, cap, keep, first,
                            recent, kept, cluster, rows);
     count_launch();

@@ -57,6 +57,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     __shared__ __align__(8) int s_vis[kCols];             // keys of the run that the row sees
     __shared__ int s_least[kCols / 32], s_most[kCols / 32];
     const int tid = threadIdx.x, warp = tid >> 5;
+    grid_dependency_wait();
     const int bh = blockIdx.x / runs, b = bh / H, h = bh - b * H, n = min(max(cache_len[bh], 0), cap);
     const int from = (blockIdx.x - bh * runs) * run, to = min(n, from + run);
     if (from >= n) return;
@@ -79,6 +80,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    launch_dependents();
     const uint32_t tmem = bar.tmem;
     volatile int *abort_flag = bar.abort;
     uint8_t *ring = dyn_u + 2 * kQHalf;
@@ -252,10 +254,10 @@ cudaError_t launch(const CUtensorMap &map_q, const CUtensorMap &map_k, const flo
     auto kernel = cache_weights_umma_kernel<G, kNorm>;
     cudaError_t e = allow_smem(kernel, kSmem);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)(BH * runs), kThreads, kSmem, st>>>(map_q, map_k, lse, visible, cache_len, cap, weight, s.H, s.L, scale, norm_eps,
-                                                           runs, run, debug_wait_kcycles());
+    e = launch_kernel(kernel, dim3((unsigned)(BH * runs)), dim3(kThreads), kSmem, st, true, map_q, map_k, lse, visible, cache_len, cap,
+                      weight, s.H, s.L, scale, norm_eps, runs, run, debug_wait_kcycles());
     count_launch();
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace

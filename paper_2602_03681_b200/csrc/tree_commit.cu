@@ -61,6 +61,8 @@ tree_commit_kernel(const ST *__restrict__ k, const ST *__restrict__ v, const flo
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[r] = S[(size_t)(row0 + 4 * q + r) * kVec];
     };
+    tc::grid_dependency_wait();
+    tc::launch_dependents();
     load(0);
 
     const int m_raw = n_path[b], m = min(max(m_raw, 0), T), n_raw = cache_len[bh], n_old = min(max(n_raw, 0), cap);
@@ -152,11 +154,11 @@ cudaError_t launch(const void *k, const void *v, const float *g, const uint8_t *
                    float norm_eps, void *ws, cudaStream_t st) {
     cudaError_t e = allow_smem(tree_commit_kernel<ST, D>, 2 * kMaxNodes * D * 4);
     if (e != cudaSuccess) return e;
-    tree_commit_kernel<ST, D><<<s.B * s.H, kCommitThreads, 2 * s.L * D * 4, st>>>(
-        (const ST *)k, (const ST *)v, g, route, u, path, n_path, state, (ST *)k_cache, (ST *)v_cache, cache_len, cap, s.H, s.L,
-        norm_eps, reinterpret_cast<int32_t *>(ws));
+    e = launch_kernel(tree_commit_kernel<ST, D>, dim3(s.B * s.H), dim3(kCommitThreads), 2 * s.L * D * 4, st, true, (const ST *)k,
+                      (const ST *)v, g, route, u, path, n_path, state, (ST *)k_cache, (ST *)v_cache, cache_len, cap, s.H, s.L, norm_eps,
+                      reinterpret_cast<int32_t *>(ws));
     count_launch();
-    return cudaGetLastError();
+    return e;
 }
 
 }  // namespace
