@@ -281,6 +281,43 @@ def test_generation_with_a_bounded_cache(dtype, G, norm):
         assert binding.natsl_device_status(ws) == 0
 
 
+@pytest.mark.parametrize("dtype,T", [("bf16", 12), ("bf16", 40), ("f32", 12)])
+def test_calls_one_behind_the_other(dtype, T):
+    """Step, weights, commit and eviction, three rounds of them: enqueued back to back (each may start while the one ahead of it
+    ends) and with the GPU waited for after each."""
+    from paper_2602_03681_b200 import binding
+    B, H, d, cap, keep = 24, 16, 128, 500, 300
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng = np.random.default_rng(T)
+    x = make(T, B, H, T, d, [0, 290, 300, 300, 299], cap, dtype, route="all")
+    t = {n: dev(x[n], dt if n in ("q", "k", "v", "k_cache", "v_cache") else None) for n in x if x[n] is not None}
+    weight = dev(rng.random((B, H, cap)).astype(np.float32))
+    la, sm = scales(d, 1, False)
+    got = []
+    for wait in (True, False, False):
+        kc, vc, w, n, state = (y.clone() for y in (t["k_cache"], t["v_cache"], weight, t["cache_len"], t["state"]))
+        out, u = torch.empty_like(t["q"]), torch.empty(B, T, H, d, device="cuda")
+        lse, kept = torch.empty(B, H, T, device="cuda"), torch.full((B, H, keep), -1, dtype=torch.int32, device="cuda")
+        p = binding.make_params(B, H, T, d, binding._dtype_code(out), la, sm, w=t["w"], lse=lse)
+        ws = binding.alloc_workspace(p, binding.OP_TREE)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for f in (lambda: binding.natsl_tree_step(t["q"], t["k"], t["v"], t["g"], t["beta"], t["route"], t["parent"], None, state, kc,
+                                                      vc, n, out, u, p, ws),
+                      lambda: binding.natsl_cache_weights(t["q"], lse, None, kc, n, w, p),
+                      lambda: binding.natsl_tree_commit(t["k"], t["v"], t["g"], t["route"], u, t["path"], t["n_path"], state, kc, vc, n,
+                                                        p, ws),
+                      lambda: binding.natsl_cache_evict(kc, vc, w, n, keep, 2, 10, kept, p)):
+                f()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert binding.natsl_device_status(ws) == 0
+        got.append([out, u, lse, state, n, kept, w, kc, vc])
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
 @pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 40), ("f32", 9)])
 def test_offsets_past_32_bits(dtype, T):
     """Caches of more than 2^31 elements a pair: the second pair's lies behind them.  All four calls give what they give for
