@@ -7,9 +7,9 @@
 // natsl_cache_evict keeps the first entries, the latest ones and the heaviest of the rest (a radix select on the
 // weights' bits finds the threshold; ties to the lowest index) and moves them to the front, in order and in place.
 //
-// B200: the weights of 64 x 16 caches of 1638 entries of 128 columns for up to 16 rows 74 us (444 MB: 6.0 TB/s, 92 % of a
+// B200: the weights of 64 x 16 caches of 1638 entries of 128 columns for up to 16 rows 72 us (444 MB: 6.2 TB/s, 94 % of a
 // copy's rate); one pass of eviction over 64 x 16 caches of 1638 150 us at its first call (up to 1.09 GB, entries before the
-// first gap stay) and 41 us where only the latest entries move; 16 caches of 8192 entries 34 us and 22 us.
+// first gap stay) and 39 us where only the latest entries move; 16 caches of 8192 entries 34 us and 20 us.
 #include <algorithm>
 #include "common.cuh"
 #include "natsl_internal.h"
@@ -110,27 +110,24 @@ cache_weights_simt_kernel(const ST *__restrict__ q, const float *__restrict__ ls
 }
 
 // ------------------------------------------------------------------------------------------
-// Weights, tensor cores (bf16 storage, one or two softmax heads per linear head; 64 columns, or up to 32 rows of 128).  Bound by
-// reading K once, up to some 64 rows.  A CTA takes a run of a pair's keys through a ring of asynchronous copies, tiles of 64,
-// and up to 64 rows of q at a time as fragments in registers (R: 16-row tiles); its warps share the tile by keys, beyond 32
-// rows also by rows.
+// Weights of up to 16 rows, tensor cores (bf16 storage, one or two softmax heads per linear head).  Bound by reading K once.  A CTA
+// takes a run of a pair's keys through a ring of asynchronous copies, tiles of 64, the rows of q as fragments in registers; its
+// warps share the tile by keys.  (More rows: cache_weights_umma.cu, which has both sides' times.)
 // ------------------------------------------------------------------------------------------
 constexpr int kTTile = 64, kTStages = 3, kMaxRun = 1024;
 
-template <int D, int G, bool kNorm, int R>
-__global__ void __launch_bounds__(kWThreads, R == 1 ? 4 : 3)
+template <int D, int G, bool kNorm>
+__global__ void __launch_bounds__(kWThreads, 4)
 cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__ lse, const int32_t *__restrict__ visible,
                         const uint8_t *__restrict__ k_cache, const int32_t *__restrict__ cache_len, int cap,
                         float *__restrict__ weight, int H, int T, float scale, float norm_eps, int runs, int run) {
-    constexpr int ds = D / G, kKs = ds / 16, kRows = 16 * R, kMt = R < 2 ? R : 2, kRowGroups = R / kMt, kKeyGroups = 4 / kRowGroups;
-    constexpr int kKeys = kTTile / kKeyGroups, kNt = kKeys / 8, kRowBytes = D * 2, kPieces = kRowBytes / 16, kStep = kWThreads / kPieces;
-    constexpr int kTileBytes = kTTile * kRowBytes;
-    extern __shared__ __align__(128) uint8_t dyn_w[];      // the ring; then the sums [row groups][run]
+    constexpr int ds = D / G, kKs = ds / 16, kRows = 16, kKeys = kTTile / 4, kNt = kKeys / 8;
+    constexpr int kRowBytes = D * 2, kPieces = kRowBytes / 16, kStep = kWThreads / kPieces, kTileBytes = kTTile * kRowBytes;
+    extern __shared__ __align__(128) uint8_t dyn_w[];      // the ring; then the sums [run]
     __shared__ float2 s_row[G][kRows];            // factor to base-2 logits, log-sum-exp in base 2
     __shared__ int s_vis[G][kRows];
     __shared__ __align__(8) float s_key[kNorm ? G : 1][kTTile];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g4 = lane >> 2, c4 = lane & 3;
-    const int rg = warp / kKeyGroups, kg = warp - rg * kKeyGroups, r0 = rg * 16 * kMt;
     tc::grid_dependency_wait();
     tc::launch_dependents();
     const int bh = blockIdx.x / runs, b = bh / H, h = bh - b * H, n = min(max(cache_len[bh], 0), cap);
@@ -152,184 +149,139 @@ cache_weights_tc_kernel(const uint8_t *__restrict__ q, const float *__restrict__
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    for (int t0 = 0; t0 < T; t0 += kRows) {
-        const int rows = min(kRows, T - t0);
-        if (t0) __syncthreads();                  // (the last tiles and rows have been read)
 #pragma unroll
-        for (int i = 0; i < kTStages - 1; ++i) fetch(i);
-        for (int e = tid; e < kRows * G; e += kWThreads) {
-            const int g = e / kRows, t = e - g * kRows;
-            int vis = 0;
-            float l = 0.f;
-            if (t < rows) {
-                l = lse[((size_t)bh * G + g) * T + t0 + t];
-                vis = visible ? max(min(visible[((size_t)b * T + t0 + t) * H + h], n), 0) : n;
-                if (!isfinite(l)) vis = 0;        // (a row that sees nothing)
-            }
-            s_vis[g][t] = vis - from;
-            s_row[g][t] = make_float2(scale * kLog2e, l * kLog2e);
+    for (int i = 0; i < kTStages - 1; ++i) fetch(i);
+    for (int e = tid; e < kRows * G; e += kWThreads) {
+        const int g = e / kRows, t = e - g * kRows;
+        int vis = 0;
+        float l = 0.f;
+        if (t < T) {
+            l = lse[((size_t)bh * G + g) * T + t];
+            vis = visible ? max(min(visible[((size_t)b * T + t) * H + h], n), 0) : n;
+            if (!isfinite(l)) vis = 0;            // (a row that sees nothing)
         }
-        // (q passes through the ring's last place, which the first tile's turn fills)
-        constexpr int kQ = (kTStages - 1) * kTileBytes;
-        for (int e = tid; e < kRows * kPieces; e += kWThreads) {
-            const int t = e / kPieces, c = e - t * kPieces;
-            *reinterpret_cast<uint4 *>(dyn_w + kQ + t * kRowBytes + ((c ^ (t & 7)) << 4)) =
-                t < rows ? *reinterpret_cast<const uint4 *>(q + (((size_t)b * T + t0 + t) * H + h) * kRowBytes + c * 16) : make_uint4(0, 0, 0, 0);
-        }
-        __syncthreads();
-        uint32_t qf[kMt][D / 16][4];
+        s_vis[g][t] = vis - from;
+        s_row[g][t] = make_float2(scale * kLog2e, l * kLog2e);
+    }
+    // (q passes through the ring's last place, which the first tile's turn fills)
+    constexpr int kQ = (kTStages - 1) * kTileBytes;
+    for (int e = tid; e < kRows * kPieces; e += kWThreads) {
+        const int t = e / kPieces, c = e - t * kPieces;
+        *reinterpret_cast<uint4 *>(dyn_w + kQ + t * kRowBytes + ((c ^ (t & 7)) << 4)) =
+            t < T ? *reinterpret_cast<const uint4 *>(q + (((size_t)b * T + t) * H + h) * kRowBytes + c * 16) : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    uint32_t qf[D / 16][4];
 #pragma unroll
-        for (int m = 0; m < kMt; ++m)
+    for (int k = 0; k < D / 16; ++k) {
+        const int t = lane & 15;
+        tc::ldmatrix_x4(ring + kQ + t * kRowBytes + (((2 * k + (lane >> 4)) ^ (t & 7)) << 4), qf[k]);
+    }
+    float2 f[G][2];
+    int vis[G][2];
+    int least = 0x7fffffff;                       // keys that all rows see
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-                const int t = r0 + m * 16 + (lane & 15);
-                tc::ldmatrix_x4(ring + kQ + t * kRowBytes + (((2 * k + (lane >> 4)) ^ (t & 7)) << 4), qf[m][k]);
-            }
-        float2 f[G][kMt][2];
-        int vis[G][kMt][2];
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    f[g][m][r] = s_row[g][r0 + m * 16 + r * 8 + g4];
-                    vis[g][m][r] = s_vis[g][r0 + m * 16 + r * 8 + g4] - kg * kKeys - 2 * c4;
-                    if (kNorm) {
-                        float ss = 0.f;
-#pragma unroll
-                        for (int k = g * kKs; k < (g + 1) * kKs; ++k)
-#pragma unroll
-                            for (int x = 0; x < 2; ++x) ss = square_sum(qf[m][k][r + 2 * x], ss);
-                        ss += __shfl_xor_sync(0xffffffffu, ss, 1);
-                        ss += __shfl_xor_sync(0xffffffffu, ss, 2);
-                        f[g][m][r].x *= rsqrtf(ss / ds + norm_eps);
-                    }
-                }
-        int least = 0x7fffffff;                   // keys that all of the warp's rows see
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) least = min(least, vis[g][m][r]);
-        least = __reduce_min_sync(0xffffffffu, least + 2 * c4);
-        for (int t = 0; t < tiles; ++t) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kTStages - 2) : "memory");
-            __syncthreads();                      // tile t is there, and every warp is done with tile t - 1 ...
-            fetch(t + kTStages - 1);              // ... whose place this one takes
-            const uint32_t kt = ring + t % kTStages * kTileBytes;
-            if (kNorm) {                          // a key's RMS factors: two threads each, half a row
-                const int key = tid >> 1, half = tid & 1;
-                const uint8_t *row = dyn_w + (kt - ring) + key * kRowBytes;
+        for (int r = 0; r < 2; ++r) {
+            f[g][r] = s_row[g][r * 8 + g4];
+            vis[g][r] = s_vis[g][r * 8 + g4] - warp * kKeys - 2 * c4;
+            least = min(least, vis[g][r]);
+            if (kNorm) {
                 float ss = 0.f;
-#pragma unroll
-                for (int i = 0; i < kPieces / 2; ++i) {
-                    const int p = half * (kPieces / 2) + ((i + 4 * half) & (kPieces / 2 - 1));
-                    const uint4 y = *reinterpret_cast<const uint4 *>(row + ((p ^ (key & 7)) << 4));
-                    ss = square_sum(y.x, square_sum(y.y, square_sum(y.z, square_sum(y.w, ss))));
-                }
-                if (G == 1) ss += __shfl_xor_sync(0xffffffffu, ss, 1);
-                s_key[G == 2 ? half : 0][key] = rsqrtf(ss / ds + norm_eps);
-                __syncthreads();
-            }
-            float sum[kNt][2];
-#pragma unroll
-            for (int i = 0; i < kNt; ++i) sum[i][0] = sum[i][1] = 0.f;
-            const bool all = (t + 1) * kTTile <= least;      // (uniform)
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                float x[kMt][kNt][4];
-#pragma unroll
-                for (int i = 0; i < kNt; ++i)
-#pragma unroll
-                    for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) x[m][i][y] = 0.f;
 #pragma unroll
                 for (int k = g * kKs; k < (g + 1) * kKs; ++k)
 #pragma unroll
-                    for (int i = 0; i < kNt; i += 2) {
-                        const int row = kg * kKeys + i * 8 + (lane & 7) + (lane >> 4) * 8;
-                        uint32_t bf[4];
-                        tc::ldmatrix_x4(kt + row * kRowBytes + (((2 * k + ((lane >> 3) & 1)) ^ (row & 7)) << 4), bf);
-#pragma unroll
-                        for (int m = 0; m < kMt; ++m) {
-                            mma_bf16(x[m][i], qf[m][k], bf[0], bf[1]);
-                            mma_bf16(x[m][i + 1], qf[m][k], bf[2], bf[3]);
-                        }
-                    }
-#pragma unroll
-                for (int i = 0; i < kNt; ++i) {
-                    float2 w = make_float2(1.f, 1.f);
-                    if (kNorm) w = *reinterpret_cast<const float2 *>(&s_key[g][kg * kKeys + i * 8 + 2 * c4]);
-#pragma unroll
-                    for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r)
-#pragma unroll
-                            for (int y = 0; y < 2; ++y) {
-                                const float z = kNorm ? x[m][i][2 * r + y] * (y ? w.y : w.x) : x[m][i][2 * r + y];
-                                x[m][i][2 * r + y] = tc::ex2_ftz(fmaf(z, f[g][m][r].x, -f[g][m][r].y));
-                            }
-                }
-                if (!all)
-#pragma unroll
-                    for (int i = 0; i < kNt; ++i)
-#pragma unroll
-                        for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                                for (int y = 0; y < 2; ++y)
-                                    if (t * kTTile + i * 8 + y >= vis[g][m][r]) x[m][i][2 * r + y] = 0.f;
-#pragma unroll
-                for (int i = 0; i < kNt; ++i)
-#pragma unroll
-                    for (int m = 0; m < kMt; ++m)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            sum[i][0] += x[m][i][2 * r];
-                            sum[i][1] += x[m][i][2 * r + 1];
-                        }
+                    for (int x = 0; x < 2; ++x) ss = square_sum(qf[k][r + 2 * x], ss);
+                ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+                ss += __shfl_xor_sync(0xffffffffu, ss, 2);
+                f[g][r].x *= rsqrtf(ss / ds + norm_eps);
             }
+        }
+    least = __reduce_min_sync(0xffffffffu, least + 2 * c4);
+    for (int t = 0; t < tiles; ++t) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kTStages - 2) : "memory");
+        __syncthreads();                          // tile t is there, and every warp is done with tile t - 1 ...
+        fetch(t + kTStages - 1);                  // ... whose place this one takes
+        const uint32_t kt = ring + t % kTStages * kTileBytes;
+        if (kNorm) {                              // a key's RMS factors: two threads each, half a row
+            const int key = tid >> 1, half = tid & 1;
+            const uint8_t *row = dyn_w + (kt - ring) + key * kRowBytes;
+            float ss = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int p = half * (kPieces / 2) + ((i + 4 * half) & (kPieces / 2 - 1));
+                const uint4 y = *reinterpret_cast<const uint4 *>(row + ((p ^ (key & 7)) << 4));
+                ss = square_sum(y.x, square_sum(y.y, square_sum(y.z, square_sum(y.w, ss))));
+            }
+            if (G == 1) ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+            s_key[G == 2 ? half : 0][key] = rsqrtf(ss / ds + norm_eps);
+            __syncthreads();
+        }
+        float sum[kNt][2];
+#pragma unroll
+        for (int i = 0; i < kNt; ++i) sum[i][0] = sum[i][1] = 0.f;
+        const bool all = (t + 1) * kTTile <= least;              // (uniform)
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            float x[kNt][4];
 #pragma unroll
             for (int i = 0; i < kNt; ++i)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
+                for (int y = 0; y < 4; ++y) x[i][y] = 0.f;
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) sum[i][y] += __shfl_xor_sync(0xffffffffu, sum[i][y], o);
-                }
-            if (g4 == 0) {                        // (a key's sums always belong to the same warp of a row group)
+            for (int k = g * kKs; k < (g + 1) * kKs; ++k)
 #pragma unroll
-                for (int i = 0; i < kNt; ++i) {
-                    float2 *at = reinterpret_cast<float2 *>(s_sum + rg * run + t * kTTile + kg * kKeys + i * 8 + 2 * c4);
-                    const float2 was = t0 ? *at : make_float2(0.f, 0.f);
-                    *at = make_float2(was.x + sum[i][0], was.y + sum[i][1]);
+                for (int i = 0; i < kNt; i += 2) {
+                    const int row = warp * kKeys + i * 8 + (lane & 7) + (lane >> 4) * 8;
+                    uint32_t bf[4];
+                    tc::ldmatrix_x4(kt + row * kRowBytes + (((2 * k + ((lane >> 3) & 1)) ^ (row & 7)) << 4), bf);
+                    mma_bf16(x[i], qf[k], bf[0], bf[1]);
+                    mma_bf16(x[i + 1], qf[k], bf[2], bf[3]);
                 }
+#pragma unroll
+            for (int i = 0; i < kNt; ++i) {
+                float2 w = make_float2(1.f, 1.f);
+                if (kNorm) w = *reinterpret_cast<const float2 *>(&s_key[g][warp * kKeys + i * 8 + 2 * c4]);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const float z = kNorm ? x[i][2 * r + y] * (y ? w.y : w.x) : x[i][2 * r + y];
+                        const float e = tc::ex2_ftz(fmaf(z, f[g][r].x, -f[g][r].y));
+                        sum[i][y] += all || t * kTTile + i * 8 + y < vis[g][r] ? e : 0.f;
+                    }
             }
         }
-        cp_async_wait_all();
+#pragma unroll
+        for (int i = 0; i < kNt; ++i)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) sum[i][y] += __shfl_xor_sync(0xffffffffu, sum[i][y], o);
+            }
+        if (g4 == 0) {
+#pragma unroll
+            for (int i = 0; i < kNt; ++i)
+                *reinterpret_cast<float2 *>(s_sum + t * kTTile + warp * kKeys + i * 8 + 2 * c4) = make_float2(sum[i][0], sum[i][1]);
+        }
     }
+    cp_async_wait_all();
     __syncthreads();
-    for (int j = tid; j < to - from; j += kWThreads) {
-        float z = s_sum[j];
-        if (kRowGroups > 1) z += s_sum[run + j];
-        weight[(size_t)bh * cap + from + j] += z;
-    }
+    for (int j = tid; j < to - from; j += kWThreads) weight[(size_t)bh * cap + from + j] += s_sum[j];
 }
 
-template <int D, int G, bool kNorm, int R>
+template <int D, int G, bool kNorm>
 cudaError_t launch_weights_tc(const void *q, const float *lse, const int32_t *visible, const void *k_cache, const int32_t *cache_len,
                               int cap, float *weight, float scale, Shape s, float norm_eps, cudaStream_t st) {
     // Runs of 128 to 1024 keys: as short as one resident set of CTAs allows.
-    const long long BH = (long long)s.B * s.H, resident = 148 * (R == 1 ? 4 : 3), per = (BH * cap + resident - 1) / resident;
+    const long long BH = (long long)s.B * s.H, resident = 148 * 4, per = (BH * cap + resident - 1) / resident;
     const int run = (int)std::min<long long>(kMaxRun, std::max<long long>(128, (per + kTTile - 1) / kTTile * kTTile));
     const int runs = (cap + run - 1) / run, ring = kTStages * kTTile * D * 2;
-    auto kernel = cache_weights_tc_kernel<D, G, kNorm, R>;
-    cudaError_t e = allow_smem(kernel, ring + 2 * kMaxRun * 4);
+    auto kernel = cache_weights_tc_kernel<D, G, kNorm>;
+    cudaError_t e = allow_smem(kernel, ring + kMaxRun * 4);
     if (e != cudaSuccess) return e;
-    e = launch_kernel(kernel, dim3((unsigned)(BH * runs)), dim3(kWThreads), ring + (R > 2 ? 2 : 1) * run * 4, st, true, (const uint8_t *)q,
+    e = launch_kernel(kernel, dim3((unsigned)(BH * runs)), dim3(kWThreads), ring + run * 4, st, true, (const uint8_t *)q,
                       lse, visible, (const uint8_t *)k_cache, cache_len, cap, weight, s.H, s.L, scale, norm_eps, runs, run);
     count_launch();
     return e;
@@ -555,12 +507,9 @@ cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t 
                                  const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg,
                                  bool tensor_cores, cudaStream_t st) {
     if (tensor_cores && hg.G <= 2) {
-        if (s.d == 128 && s.L > 32) return launch_weights_umma(q, lse, visible, k_cache, cache_len, cap, weight, scale, s, hg, st);
+        if (s.L > 16) return launch_weights_umma(q, lse, visible, k_cache, cache_len, cap, weight, scale, s, hg, st);
 #define ARGS q, lse, visible, k_cache, cache_len, cap, weight, scale, s, hg.norm_eps, st
-#define BY_ROWS(D, G, N)                                                                                                   \
-    return s.L <= 16 ? launch_weights_tc<D, G, N, 1>(ARGS)                                                                 \
-                     : s.L <= 32 || D == 128 ? launch_weights_tc<D, G, N, 2>(ARGS) : launch_weights_tc<D, G, N, D == 128 ? 2 : 4>(ARGS)
-#define BY_NORM(D, G) do { if (hg.norm_eps >= 0.f) BY_ROWS(D, G, true); BY_ROWS(D, G, false); } while (0)
+#define BY_NORM(D, G) return hg.norm_eps >= 0.f ? launch_weights_tc<D, G, true>(ARGS) : launch_weights_tc<D, G, false>(ARGS)
         if (s.d == 128) {
             if (hg.G == 2) BY_NORM(128, 2);
             BY_NORM(128, 1);
@@ -568,7 +517,6 @@ cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t 
         if (hg.G == 2) BY_NORM(64, 2);
         BY_NORM(64, 1);
 #undef BY_NORM
-#undef BY_ROWS
 #undef ARGS
     }
     const int blocks = (cap + kWKeys - 1) / kWKeys;

@@ -1,13 +1,17 @@
-// Attention weight of the retained entries for more than 32 query rows of 128 columns: the transposed logits K q^T as tcgen05
-// MMAs, so that a thread has a key, its sum over the rows needs no neighbour and the key's RMS factor is a register.
+// Attention weight of the retained entries for more than 16 query rows (bf16 storage, one or two softmax heads): the transposed
+// logits K q^T as tcgen05 MMAs, so that a thread has a key, its sum over the rows needs no neighbour and the key's RMS factor is
+// a register.
 //
 //   weight_j += sum_t sum_s exp2(f_ts k_js.q_ts - l_ts),   f = scale log2(e) (/ RMS(q)), l = lse log2(e)
 //
 // Bound by memory up to some 64 exponentials a key, then by those: a multiprocessor takes 11 cycles to get a key's 256 bytes and
-// one for 16 exponentials.  Two CTAs per multiprocessor, each with 64 rows of q at a time as the B operand and a ring of five half
-// tiles of K (128 keys, 64 columns: with two softmax heads, a head's).  Two groups of four warps take tiles in turns; one warp
-// issues copies, one MMAs.  B200: 64 rows, two heads, 4 x 16 caches of up to 3277 keys 22.6 us, where warp-level MMAs took
-// 26.7: of a CTA's 24000 cycles 12300 are the exponentials of its multiprocessor, 4000 the start up to the rows' factors.
+// one for 16 exponentials.  Two CTAs per multiprocessor, each with 64 rows of q at a time as the B operand and a ring of five
+// slices of K (128 keys, 64 columns).  Two groups of four warps take tiles in turns; one warp issues copies, one MMAs.
+//
+// B200: 64 rows, two heads, 4 x 16 caches of up to 3277 keys 20 us: of a CTA's 24000 cycles 12300 are the exponentials of its
+// multiprocessor, 4000 the start up to the rows' factors.  Against warp-level MMAs with the rows in registers, 64 x 16 caches of
+// up to 1638 keys of 128 columns, one head / two normalised: 16 rows 62 / 80 us where those take 59 / 70; 17 rows 62 / 80 and
+// 70 / 99, 64 rows 65 / 106 and 92 / 135, 128 rows 107 / 201 and 171 / 258.
 #include <algorithm>
 #include "common.cuh"
 #include "natsl_internal.h"
@@ -19,9 +23,8 @@ namespace {
 using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kRows = 64, kKeys = 128, kStages = 5, kHalfTile = kKeys * 128, kQHalf = kRows * 128;
+constexpr int kRows = 64, kKeys = 128, kStages = 5, kSlice = kKeys * 128, kQSlice = kRows * 128;      // (slices: 64 columns)
 constexpr int kWorkers = 256, kThreads = kWorkers + 64;
-constexpr int kSmem = 2 * kQHalf + kStages * kHalfTile;
 
 struct Bars {
     uint64_t full[kStages], empty[kStages], q_full, q_empty, s[4], free[4], drain;
@@ -33,25 +36,24 @@ __device__ __forceinline__ float square_sum(uint32_t bf16x2, float s) {
     const float lo = __uint_as_float(bf16x2 << 16), hi = __uint_as_float(bf16x2 & 0xffff0000u);
     return fmaf(lo, lo, fmaf(hi, hi, s));
 }
-// Sum of squares of 64 columns of row r (rows of 128 bytes, 16-byte pieces swizzled by row).
-__device__ __forceinline__ float row_squares(const uint8_t *half, int r) {
-    float ss = 0.f;
+// ss[head] += the squares of row r of slice c (rows of 128 bytes, 16-byte pieces swizzled by row).
+template <int D, int G> __device__ __forceinline__ void row_squares(const uint8_t *slice, int c, int r, float (&ss)[G]) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const uint4 y = *reinterpret_cast<const uint4 *>(half + r * 128 + ((c ^ (r & 7)) << 4));
-        ss = square_sum(y.x, square_sum(y.y, square_sum(y.z, square_sum(y.w, ss))));
+    for (int i = 0; i < 8; ++i) {
+        const uint4 y = *reinterpret_cast<const uint4 *>(slice + r * 128 + ((i ^ (r & 7)) << 4));
+        float &s = ss[(c * 64 + i * 8) / (D / G)];
+        s = square_sum(y.x, square_sum(y.y, square_sum(y.z, square_sum(y.w, s))));
     }
-    return ss;
 }
 
-template <int G, bool kNorm>
+template <int D, int G, bool kNorm>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                           const float *__restrict__ lse, const int32_t *__restrict__ visible, const int32_t *__restrict__ cache_len,
                           int cap, float *__restrict__ weight, int H, int T, float scale, float norm_eps, int runs, int run,
                           int wait_kcycles) {
-    constexpr int ds = 128 / G, kCols = kRows * G;        // columns of a tile's logits
-    extern __shared__ __align__(1024) uint8_t dyn_u[];    // q: two halves; then the ring
+    constexpr int ds = D / G, kSlices = D / 64, kCols = kRows * G;       // kCols: columns of a tile's logits
+    extern __shared__ __align__(1024) uint8_t dyn_u[];    // q, slice by slice; then the ring
     __shared__ Bars bar;
     __shared__ __align__(16) float2 s_row[kCols];         // factor to base-2 logits, log-sum-exp in base 2
     __shared__ __align__(8) int s_vis[kCols];             // keys of the run that the row sees
@@ -83,24 +85,24 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     launch_dependents();
     const uint32_t tmem = bar.tmem;
     volatile int *abort_flag = bar.abort;
-    uint8_t *ring = dyn_u + 2 * kQHalf;
+    uint8_t *ring = dyn_u + kSlices * kQSlice;
     const int tiles = (to - from + kKeys - 1) / kKeys, chunks = (T + kRows - 1) / kRows;
-    // Tiles are counted through the chunks of rows: u = chunk tiles + tile; half tile 2 u + c.
+    // Tiles are counted through the chunks of rows: u = chunk tiles + tile; slice kSlices u + c.
     auto place_of = [](int u) { return (u & 1) * 2 + (G == 1 ? (u >> 1) & 1 : 0); };         // of the logits, 64 columns each
     auto place_phase = [](int u) { return (uint32_t)(G == 1 ? u >> 2 : u >> 1) & 1; };
 
     if (tid >= kWorkers + 32) {                   // ---- copies ----
         const int nt = (int)uniform((uint32_t)tiles), all = nt * (int)uniform((uint32_t)chunks);
-        int i = 0, q = 0;                         // half tiles and chunks of q asked for
+        int i = 0, q = 0;                         // slices and chunks of q asked for
         bool ok = true;
-        for (; i < 2 * all; ++i) {
-            const int u = i >> 1, t = u % nt, s = i % kStages;
-            if (t == 0 && !(i & 1)) {
+        for (; i < kSlices * all; ++i) {
+            const int u = i / kSlices, t = u % nt, s = i % kStages;
+            if (t == 0 && i % kSlices == 0) {
                 ok = q == 0 || wait_all(&bar.q_empty, (q - 1) & 1, abort_flag);
                 if (!ok) break;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&bar.q_full, 2 * kQHalf);
-                    for (int c = 0; c < 2; ++c) tma_load_4d(dyn_u + c * kQHalf, &map_q, &bar.q_full, c * 64, h, q * kRows, b);
+                    mbar_arrive_expect_tx(&bar.q_full, kSlices * kQSlice);
+                    for (int c = 0; c < kSlices; ++c) tma_load_4d(dyn_u + c * kQSlice, &map_q, &bar.q_full, c * 64, h, q * kRows, b);
                 }
                 ++q;
                 __syncwarp();
@@ -108,8 +110,8 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             ok = i < kStages || wait_all(&bar.empty[s], (i / kStages - 1) & 1, abort_flag);
             if (!ok) break;
             if (elect_one()) {
-                mbar_arrive_expect_tx(&bar.full[s], kHalfTile);
-                tma_load_2d(ring + s * kHalfTile, &map_k, &bar.full[s], (i & 1) * 64, bh * cap + from + t * kKeys);
+                mbar_arrive_expect_tx(&bar.full[s], kSlice);
+                tma_load_2d(ring + s * kSlice, &map_k, &bar.full[s], i % kSlices * 64, bh * cap + from + t * kKeys);
             }
             __syncwarp();
         }
@@ -128,18 +130,19 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             if (u >= (G == 1 ? 4 : 2)) ok = ok && wait_all(&bar.free[place], place_phase(u) ^ 1, abort_flag);
             tc_fence_after_sync();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int i = 2 * u + c, s = i % kStages;
+            for (int c = 0; c < kSlices; ++c) {
+                const int i = kSlices * u + c, s = i % kStages;
                 ok = ok && wait_all(&bar.full[s], (i / kStages) & 1, abort_flag);
                 if (!ok) break;
-                const uint32_t ak = uniform(smem_u32(ring + s * kHalfTile)), ts = tm + 64 * place + (G == 2 ? 64 * c : 0);
+                const uint32_t ak = uniform(smem_u32(ring + s * kSlice)), ts = tm + 64 * place;
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        mma_ss(ts, desc_kmajor(ak + k * 32), desc_kmajor(aq + c * kQHalf + k * 32), idesc, G == 2 ? k != 0 : (c | k) != 0);
+                        mma_ss(ts + (c * 64 + k * 16) / ds * 64, desc_kmajor(ak + k * 32), desc_kmajor(aq + c * kQSlice + k * 32), idesc,
+                               (c * 64 + k * 16) % ds != 0);
                     mma_commit(&bar.empty[s]);
-                    if (c) mma_commit(&bar.s[place]);
-                    if (c && t == nt - 1) mma_commit(&bar.q_empty);
+                    if (c == kSlices - 1) mma_commit(&bar.s[place]);
+                    if (c == kSlices - 1 && t == nt - 1) mma_commit(&bar.q_empty);
                 }
                 __syncwarp();
             }
@@ -170,9 +173,10 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 }
                 if (kNorm) {
                     ok = wait_all(&bar.q_full, chunk & 1, abort_flag) && ok;
-                    float ss = row_squares(dyn_u + (G == 2 ? s : 0) * kQHalf, t);
-                    if (G == 1) ss += row_squares(dyn_u + kQHalf, t);
-                    f *= rsqrtf(ss / ds + norm_eps);
+                    float ss[G] = {};
+#pragma unroll
+                    for (int c = 0; c < kSlices; ++c) row_squares<D, G>(dyn_u + c * kQSlice, c, t, ss);
+                    f *= rsqrtf(ss[G == 2 ? s : 0] / ds + norm_eps);
                     mbar_arrive(&bar.q_empty);
                 }
                 s_row[tid] = make_float2(f, l * kLog2e);
@@ -189,16 +193,16 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                 const float was = mine ? *at : 0.f;
                 float fk[G];
                 if (kNorm) {
-                    float ss[2];
+                    float ss[G] = {};
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int i = 2 * u + c;
+                    for (int c = 0; c < kSlices; ++c) {
+                        const int i = kSlices * u + c;
                         ok = ok && wait_all(&bar.full[i % kStages], (i / kStages) & 1, abort_flag);
-                        ss[c] = row_squares(ring + i % kStages * kHalfTile, r);
+                        row_squares<D, G>(ring + i % kStages * kSlice, c, r, ss);
                         mbar_arrive(&bar.empty[i % kStages]);
                     }
 #pragma unroll
-                    for (int s = 0; s < G; ++s) fk[s] = rsqrtf((G == 1 ? ss[0] + ss[1] : ss[s]) / ds + norm_eps);
+                    for (int s = 0; s < G; ++s) fk[s] = rsqrtf(ss[s] / ds + norm_eps);
                 }
                 ok = ok && wait_all(&bar.s[place_of(u)], place_phase(u), abort_flag);
                 tc_fence_after_sync();
@@ -244,14 +248,15 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
     }
 }
 
-template <int G, bool kNorm>
+template <int D, int G, bool kNorm>
 cudaError_t launch(const CUtensorMap &map_q, const CUtensorMap &map_k, const float *lse, const int32_t *visible,
                    const int32_t *cache_len, int cap, float *weight, float scale, Shape s, float norm_eps, cudaStream_t st) {
     // Runs of 256 to 2048 keys: as short as one resident set of CTAs allows.
     const long long BH = (long long)s.B * s.H, resident = 148 * 2, per = (BH * cap + resident - 1) / resident;
     const int run = (int)std::min<long long>(2048, std::max<long long>(256, (per + kKeys - 1) / kKeys * kKeys));
     const int runs = (cap + run - 1) / run;
-    auto kernel = cache_weights_umma_kernel<G, kNorm>;
+    constexpr int kSmem = D / 64 * kQSlice + kStages * kSlice;
+    auto kernel = cache_weights_umma_kernel<D, G, kNorm>;
     cudaError_t e = allow_smem(kernel, kSmem);
     if (e != cudaSuccess) return e;
     e = launch_kernel(kernel, dim3((unsigned)(BH * runs)), dim3(kThreads), kSmem, st, true, map_q, map_k, lse, visible, cache_len, cap,
@@ -265,11 +270,12 @@ cudaError_t launch(const CUtensorMap &map_q, const CUtensorMap &map_k, const flo
 cudaError_t launch_weights_umma(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
                                 const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg, cudaStream_t st) {
     CUtensorMap map_q, map_k;
-    if (!tch::make_map_blhd(&map_q, q, s.B, s.L, s.H, 128, kRows) ||
-        !tch::make_map_2d(&map_k, k_cache, (uint64_t)s.B * s.H * cap, 128, kKeys))
+    if (!tch::make_map_blhd(&map_q, q, s.B, s.L, s.H, s.d, kRows) ||
+        !tch::make_map_2d(&map_k, k_cache, (uint64_t)s.B * s.H * cap, s.d, kKeys))
         return cudaErrorInvalidValue;
     const bool norm = hg.norm_eps >= 0.f;
-    auto run = hg.G == 2 ? norm ? launch<2, true> : launch<2, false> : norm ? launch<1, true> : launch<1, false>;
+    auto run = s.d == 128 ? hg.G == 2 ? norm ? launch<128, 2, true> : launch<128, 2, false> : norm ? launch<128, 1, true> : launch<128, 1, false>
+                          : hg.G == 2 ? norm ? launch<64, 2, true> : launch<64, 2, false> : norm ? launch<64, 1, true> : launch<64, 1, false>;
     return run(map_q, map_k, lse, visible, cache_len, cap, weight, scale, s, hg.norm_eps, st);
 }
 

@@ -368,7 +368,7 @@ cudaError_t launch_tree_commit(const void *k, const void *v, const float *g, con
 cudaError_t launch_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
                                  const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg,
                                  bool tensor_cores, cudaStream_t st);
-// cache_weights_umma.cu: bf16 storage, d = 128, one or two softmax heads
+// cache_weights_umma.cu: bf16 storage, one or two softmax heads
 cudaError_t launch_weights_umma(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
                                 const int32_t *cache_len, int cap, float *weight, float scale, Shape s, HeadGroups hg, cudaStream_t st);
 cudaError_t launch_cache_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first,

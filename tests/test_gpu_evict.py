@@ -73,7 +73,7 @@ def case(seed, B, H, T, d, lengths, cap, dtype, G=1, norm=False):
     ("f32", 64, 1, False, 0), ("f32", 64, 2, True, 0), ("f32", 128, 4, True, 0), ("f32", 128, 2, False, 0),
     ("bf16", 64, 1, False, 0), ("bf16", 64, 2, True, 0), ("bf16", 128, 1, True, 0), ("bf16", 128, 2, True, 0),
     ("bf16", 128, 2, False, 0), ("bf16", 128, 4, True, 0), ("bf16", 128, 1, False, 1), ("bf16", 128, 1, False, 0)])
-@pytest.mark.parametrize("T", [1, 13, 64, 77])
+@pytest.mark.parametrize("T", [1, 13, 16, 17, 64, 77])
 def test_weights(dtype, d, G, norm, flags, T):
     weigh(case(T + d, 2, 3, T, d, [0, 1, 65, 200, 310, 64], 310, dtype, G, norm), dtype, G, norm, flags)
 
@@ -86,11 +86,12 @@ def test_weights_of_every_length(dtype, T):
     weigh(x, dtype, visible=False)
 
 
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G,norm", [(1, False), (1, True), (2, False), (2, True)])
-@pytest.mark.parametrize("T", [33, 65, 128, 200])
-def test_weights_of_many_rows(G, norm, T):
+@pytest.mark.parametrize("T", [32, 65, 128, 200])
+def test_weights_of_many_rows(d, G, norm, T):
     """Rows by the 64, keys by the 128, runs of 256 and more of them."""
-    x = case(T, 2, 2, T, 128, [1200, 0, 129, 256, 640], 1200, "bf16", G, norm)
+    x = case(T, 2, 2, T, d, [1200, 0, 129, 256, 640], 1200, "bf16", G, norm)
     weigh(x, "bf16", G, norm)
     weigh(x, "bf16", G, norm, visible=False)
 
@@ -101,11 +102,10 @@ def test_weights_of_many_pairs():
     weigh(x, "bf16")
 
 
-@pytest.mark.parametrize("dtype,T", [("f32", 9), ("bf16", 9), ("bf16", 70)])
-def test_rows_that_count_for_nothing(dtype, T):
+@pytest.mark.parametrize("dtype,T,d", [("f32", 9, 64), ("bf16", 9, 64), ("bf16", 70, 64), ("bf16", 70, 128)])
+def test_rows_that_count_for_nothing(dtype, T, d):
     """A row whose log-sum-exp is not finite, whatever its query holds; entries behind the length, whatever they hold; an
     entry that is NaN gets a NaN of its own."""
-    d = 64 if T < 32 else 128
     x = case(4, 1, 2, T, d, [50, 17], 60, dtype)
     x["visible"][:] = 60
     x["lse"] = logits(x, d ** 0.5, 1, False)
