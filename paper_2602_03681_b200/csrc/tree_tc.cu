@@ -59,12 +59,12 @@ template <int D, int R> struct Layout {
     // tile's keys.  Beyond 32 nodes of 128 columns the cache's products are tcgen05 MMAs: four warps of softmax and four that issue
     // the copies of K and V and the two products, beside eight for the tree's own part.  (The same for 17 to 32 nodes, with one
     // softmax warp a CTA: 224 us where warp-level MMAs take 216.)
-    static constexpr bool kUmma = R == 4 && D == 128;
+    static constexpr bool kUmma = R == 4;
     static constexpr int kCtas = R == 4 ? 1 : 2, kWarps = R == 4 ? 8 : 4;      // kWarps: of the tree's part
     static constexpr int kHalf = 32 * kWarps, kReaders = kUmma ? 256 : kHalf, kThreads = kReaders + kHalf;
     static constexpr int kKeyGroups = kUmma ? 2 : kWarps / R, kWarpKeys = kTileKeys / kKeyGroups;
     static constexpr int kRowBytes = D * 2, kTileBytes = kTileKeys * kRowBytes;
-    static constexpr int kSlots = kUmma ? 7 : R == 4 ? 8 : D == 128 ? 4 : 6;
+    static constexpr int kSlots = kUmma ? D == 128 ? 7 : 12 : D == 128 ? 4 : 6;
     static constexpr int kAccPitch = D + 4;
     static constexpr int kCols = D / 2;                      // columns of a CTA, at most
     static constexpr int kPitch = kRowBytes + 16;            // (an odd number of 16-byte pieces: eight rows, eight banks)
@@ -84,7 +84,7 @@ template <int D, int R> struct Layout {
     static constexpr int kMerge = kKeyGroups * kRows * kAccPitch * 4;
     static_assert(kMerge <= kRing, "the key groups' results lie in the ring");
     static constexpr int kTotal = oRing + kRing;
-    static_assert(!kUmma || kTotal + 8192 <= 232448, "an SM's shared memory, with the static part");
+    static_assert(!kUmma || kTotal + 9216 <= 232448, "a multiprocessor's shared memory, with the static part");
 };
 
 // The CTA's share of the cache: units 0, 1, 2, ... are K of tile 0, V of tile 0, K of tile 1, ...
@@ -342,30 +342,37 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
 // MMAs take 256 cycles; with warp-level MMAs a tile of 64 rows took 2900, twice the time that its bytes need.
 // ------------------------------------------------------------------------------------------
 struct UmmaBars {
-    uint64_t full[2][4], empty[2][4];             // [K, V][stage]
+    uint64_t full[2][6], empty[2][6];             // [K, V][stage]
     uint64_t s[4], p[4], o[4], drain[2];          // per place of logits: logits there, probabilities there, product done
     uint32_t tmem;
     int abort[2];
 };
-constexpr int kStagesK = 4, kStagesV = 3;         // (K is read twice where keys are normalised)
-__host__ __device__ constexpr int stages_of(int kv) { return kv ? kStagesV : kStagesK; }
 constexpr int kTmemCols = 512, kTmemO = 256;      // logits: four places of 64 columns; then the two groups' sums
 
-static_assert(kStagesK + kStagesV == Layout<128, 4>::kSlots, "");
-
-struct UmmaShare {
+template <int D> struct UmmaShare {
+    using L = Layout<D, 4>;
+    static constexpr int kStagesV = L::kSlots / 2, kStagesK = L::kSlots - kStagesV;      // (K is read twice if normalised)
+    static constexpr int kSlices = D / 64, kSlice = kTileKeys * 128;                     // of 64 columns
+    static_assert(kStagesK <= 6, "");
     const CUtensorMap *map[2];
     UmmaBars *bar;
     uint8_t *sm, *ring;
     int row, keys, tiles;                         // first row, keys, tiles of the share
+    static __device__ constexpr int stages(int kv) { return kv ? kStagesV : kStagesK; }
     __device__ int stage(int kv, int t) const { return kv ? t % kStagesV : t % kStagesK; }
     __device__ uint32_t phase(int kv, int t) const { return (kv ? t / kStagesV : t / kStagesK) & 1; }
-    __device__ uint8_t *at(int kv, int t) const { return ring + (kv * kStagesK + stage(kv, t)) * (kTileKeys * 256); }
+    __device__ uint8_t *at(int kv, int t) const { return ring + (kv * kStagesK + stage(kv, t)) * L::kTileBytes; }
+};
+// A head's sums: with 64 columns and two heads both get all columns (an operand of 32 would start inside the swizzle).
+template <int D, int G> struct UmmaSums {
+    static constexpr int kCols = D == 128 ? 128 / G : 64;
+    static __device__ constexpr int at(int s) { return kCols * s + (D == 128 ? 0 : s * (D / G)); }       // of its own columns
 };
 
 __device__ __forceinline__ void umma_init(UmmaBars *bar, bool norm, int wait_kcycles) {      // (one thread)
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < 6; ++s)
         for (int kv = 0; kv < 2; ++kv) { tc::mbar_init(&bar->full[kv][s], 1); tc::mbar_init(&bar->empty[kv][s], kv == 0 && norm ? 65 : 1); }
+    for (int s = 0; s < 4; ++s) {
         tc::mbar_init(&bar->s[s], 1);
         tc::mbar_init(&bar->p[s], 64);
         tc::mbar_init(&bar->o[s], 1);
@@ -381,17 +388,17 @@ template <int G> __device__ __forceinline__ uint32_t place_phase(int t) { return
 
 // The issuing warps.  One that did all four took 2600 cycles a tile, half of them for issuing itself: 145 us where four take 92.
 // Copies of K (0) or V (1).
-__device__ void umma_load(const UmmaShare &in, int kv) {
+template <int D> __device__ void umma_load(const UmmaShare<D> &in, int kv) {
     using namespace tc;
     UmmaBars *bar = in.bar;
-    const int tiles = (int)uniform((uint32_t)in.tiles), stages = stages_of(kv);
+    const int tiles = (int)uniform((uint32_t)in.tiles), stages = in.stages(kv);
     int t = 0;
     for (; t < tiles; ++t) {
         const int s = in.stage(kv, t);
         if (t >= stages && !wait_all(&bar->empty[kv][s], in.phase(kv, t) ^ 1, bar->abort)) break;
         if (elect_one()) {
-            mbar_arrive_expect_tx(&bar->full[kv][s], kTileKeys * 256);
-            for (int c = 0; c < 2; ++c) tma_load_2d(in.at(kv, t) + c * kTileKeys * 128, in.map[kv], &bar->full[kv][s], c * 64, in.row + t * kTileKeys);
+            mbar_arrive_expect_tx(&bar->full[kv][s], UmmaShare<D>::L::kTileBytes);
+            for (int c = 0; c < in.kSlices; ++c) tma_load_2d(in.at(kv, t) + c * in.kSlice, in.map[kv], &bar->full[kv][s], c * 64, in.row + t * kTileKeys);
         }
         __syncwarp();
     }
@@ -408,8 +415,8 @@ __device__ __forceinline__ void umma_drain(uint64_t *bar) {              // no M
 }
 
 // Logits = q K^T into a tile's place, once the product that read the probabilities of the place's last tile is done.
-template <int G>
-__device__ void umma_logits(const UmmaShare &in, uint32_t tmem, uint32_t q_at) {
+template <int D, int G>
+__device__ void umma_logits(const UmmaShare<D> &in, uint32_t tmem, uint32_t q_at) {
     using namespace tc;
     UmmaBars *bar = in.bar;
     constexpr uint32_t idesc = make_idesc(kFmtBF16, 128, kTileKeys, false, false);
@@ -425,11 +432,11 @@ __device__ void umma_logits(const UmmaShare &in, uint32_t tmem, uint32_t q_at) {
         const uint32_t ak = uniform(smem_u32(in.at(0, t))), a0 = aq - (t & 1) * (64 * 128), ts = tm + 64 * place;
         if (elect_one()) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < in.kSlices; ++c)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    mma_ss(ts + (G == 2 ? 64 * c : 0), desc_kmajor(a0 + c * (64 * 128) + k * 32), desc_kmajor(ak + c * (kTileKeys * 128) + k * 32),
-                           idesc, G == 2 ? k != 0 : (c | k) != 0);
+                    mma_ss(ts + (c * 64 + k * 16) / (D / G) * 64, desc_kmajor(a0 + c * (64 * 128) + k * 32), desc_kmajor(ak + c * in.kSlice + k * 32),
+                           idesc, (c * 64 + k * 16) % (D / G) != 0);
             mma_commit(&bar->s[place]);
             mma_commit(&bar->empty[0][in.stage(0, t)]);
         }
@@ -439,11 +446,12 @@ __device__ void umma_logits(const UmmaShare &in, uint32_t tmem, uint32_t q_at) {
 }
 
 // The group's sums += probabilities V.
-template <int G>
-__device__ void umma_sums(const UmmaShare &in, uint32_t tmem) {
+template <int D, int G>
+__device__ void umma_sums(const UmmaShare<D> &in, uint32_t tmem) {
     using namespace tc;
     UmmaBars *bar = in.bar;
-    constexpr uint32_t idesc = make_idesc(kFmtBF16, 128, 128 / G, false, true);
+    constexpr int kCols = UmmaSums<D, G>::kCols;
+    constexpr uint32_t idesc = make_idesc(kFmtBF16, 128, kCols, false, true);
     const int tiles = (int)uniform((uint32_t)in.tiles);
     const uint32_t tm = uniform(tmem);
     bool ok = true;
@@ -458,7 +466,7 @@ __device__ void umma_sums(const UmmaShare &in, uint32_t tmem) {
             for (int s = 0; s < G; ++s)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    mma_ts(to + 64 * s, ts + 64 * s + k * 8, desc_mnmajor(av + s * (kTileKeys * 128) + k * 2048, kTileKeys * 128), idesc,
+                    mma_ts(to + kCols * s, ts + 64 * s + k * 8, desc_mnmajor(av + (D == 128 ? s * in.kSlice : 0) + k * 2048, in.kSlice), idesc,
                            t > 1 || k != 0);
             mma_commit(&bar->o[place]);
             mma_commit(&bar->empty[1][in.stage(1, t)]);
@@ -469,36 +477,35 @@ __device__ void umma_sums(const UmmaShare &in, uint32_t tmem) {
 }
 
 // The four softmax warps: thread = row of a key group.
-template <int G, bool kNorm>
-__device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, const UmmaShare &in, uint32_t tmem, int n_nodes) {
+template <int D, int G, bool kNorm>
+__device__ void umma_softmax(const Args &a, typename Layout<D, 4>::S *sums, const UmmaShare<D> &in, uint32_t tmem, int n_nodes) {
     using namespace tc;
-    using L = Layout<128, 4>;
-    constexpr int ds = 128 / G;
+    using L = Layout<D, 4>;
+    constexpr int ds = D / G, kSlices = D / 64;
     __shared__ float s_m[G][2][64], s_z[G][2][64];
     __shared__ __align__(16) float s_rk[kNorm ? 2 : 1][2][G][64];      // [group][in turns]: the keys' RMS factors
     UmmaBars *bar = in.bar;
     volatile int *abort_flag = bar->abort;
     const int tid = threadIdx.x, warp = tid >> 5, g = warp >> 1, r = tid & 63;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16, to = tmem + kTmemO + 128 * g + lanes;
-    auto row_squares = [&](const uint8_t *tile, int row) {               // of 64 columns
-        float ss = 0.f;
+    auto row_squares = [&](const uint8_t *slice, int x, int row, float (&ss)[G]) {       // += those of slice x
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-            const uint4 y = *reinterpret_cast<const uint4 *>(tile + row * 128 + ((c ^ (row & 7)) << 4));
+            const uint4 y = *reinterpret_cast<const uint4 *>(slice + row * 128 + ((c ^ (row & 7)) << 4));
             const float2 y0 = bf2(y.x), y1 = bf2(y.y), y2 = bf2(y.z), y3 = bf2(y.w);
-            ss += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
+            ss[(x * 64 + c * 8) / ds] += y0.x * y0.x + y0.y * y0.y + y1.x * y1.x + y1.y * y1.y + y2.x * y2.x + y2.y * y2.y + y3.x * y3.x + y3.y * y3.y;
         }
-        return ss;
     };
     float f[G], m[G], z[G];
     {
-        float ss[2] = {0.f, 0.f};
+        float ss[G] = {};
         if (kNorm)
-            for (int c = 0; c < 2; ++c) ss[c] = row_squares(in.sm + L::oQ + c * (64 * 128), r);
+#pragma unroll
+            for (int c = 0; c < kSlices; ++c) row_squares(in.sm + L::oQ + c * (64 * 128), c, r, ss);
 #pragma unroll
         for (int s = 0; s < G; ++s) {
             f[s] = a.scale_sm * kLog2e;
-            if (kNorm) f[s] *= rsqrtf((G == 1 ? ss[0] + ss[1] : ss[s]) / ds + a.norm_eps);
+            if (kNorm) f[s] *= rsqrtf(ss[s] / ds + a.norm_eps);
             m[s] = -INFINITY;
             z[s] = 0.f;
         }
@@ -511,12 +518,11 @@ __device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, co
         if (kNorm) {                              // (the barrier below is everyone's, however the waits end)
             ok = ok && wait_all(&bar->full[0][in.stage(0, t)], in.phase(0, t), abort_flag);
             if (ok) {
-                const uint8_t *tile = in.at(0, t);
-                float ss[2];
+                float ss[G] = {};
 #pragma unroll
-                for (int c = 0; c < 2; ++c) ss[c] = row_squares(tile + c * (kTileKeys * 128), r);
+                for (int c = 0; c < kSlices; ++c) row_squares(in.at(0, t) + c * in.kSlice, c, r, ss);
 #pragma unroll
-                for (int s = 0; s < G; ++s) s_rk[g][i & 1][s][r] = rsqrtf((G == 1 ? ss[0] + ss[1] : ss[s]) / ds + a.norm_eps);
+                for (int s = 0; s < G; ++s) s_rk[g][i & 1][s][r] = rsqrtf(ss[s] / ds + a.norm_eps);
                 mbar_arrive(&bar->empty[0][in.stage(0, t)]);
             }
             named_barrier_sync(3 + g, 64);
@@ -574,11 +580,11 @@ __device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, co
 #pragma unroll 1
                     for (int c = 0; c < ds; c += 32) {
                         uint32_t o[32];
-                        tmem_ld32(to + s * ds + c, o);
+                        tmem_ld32(to + UmmaSums<D, G>::at(s) + c, o);
                         tmem_wait_ld();
 #pragma unroll
                         for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * e);
-                        tmem_st32(to + s * ds + c, o);
+                        tmem_st32(to + UmmaSums<D, G>::at(s) + c, o);
                     }
                 }
             }
@@ -588,8 +594,10 @@ __device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, co
             ok = wait_all(&bar->full[1][in.stage(1, t)], in.phase(1, t), abort_flag);
             if (ok) {
                 uint8_t *tile = in.at(1, t);
-                for (int e = r; e < (kTileKeys - left) * 16; e += 64)
-                    *reinterpret_cast<uint4 *>(tile + (e & 1) * (kTileKeys * 128) + (left + (e >> 4)) * 128 + ((e >> 1) & 7) * 16) = make_uint4(0, 0, 0, 0);
+                for (int e = r; e < (kTileKeys - left) * (D / 8); e += 64) {
+                    const int c = e % (D / 8), j = left + e / (D / 8);
+                    *reinterpret_cast<uint4 *>(tile + c / 8 * in.kSlice + j * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+                }
                 fence_proxy_async_smem();
             }
         }
@@ -602,10 +610,10 @@ __device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, co
     named_barrier_sync(1, 128);                   // (both groups' tiles have been read: the ring is free)
     float *acc = reinterpret_cast<float *>(in.ring), *mine = acc + (g * 64 + r) * L::kAccPitch;
 #pragma unroll 1
-    for (int c = 0; c < 128; c += 32) {
+    for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
         if (i > 0) {                              // (uniform)
-            tmem_ld32(to + c, o);
+            tmem_ld32(to + UmmaSums<D, G>::at(c / ds) + c % ds, o);
             tmem_wait_ld();
         } else {
 #pragma unroll
@@ -619,7 +627,7 @@ __device__ void umma_softmax(const Args &a, typename Layout<128, 4>::S *sums, co
 #pragma unroll
     for (int s = 0; s < G; ++s) { s_m[s][g][r] = m[s]; s_z[s][g][r] = z[s]; }
     named_barrier_sync(1, 128);
-    merge_groups<128, G, 4>(sums, acc, &s_m[0][0][0], &s_z[0][0][0], n_nodes, tid, 128);
+    merge_groups<D, G, 4>(sums, acc, &s_m[0][0][0], &s_z[0][0][0], n_nodes, tid, 128);
 }
 
 // x as three bf16 terms, pairwise packed: what two rounded terms leave over is exact in the third.
@@ -1051,19 +1059,19 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant_
         tc::tc_fence_after_sync();
         const uint32_t tmem = bars.tmem;
         const int keys = share.to - share.from;
-        const UmmaShare u{{&map_k, &map_v}, &bars, dyn_tc, dyn_tc + L::oRing, bh * a.cap + share.from, keys, (keys + kTileKeys - 1) / kTileKeys};
+        const UmmaShare<D> u{{&map_k, &map_v}, &bars, dyn_tc, dyn_tc + L::oRing, bh * a.cap + share.from, keys, (keys + kTileKeys - 1) / kTileKeys};
         if (tid < 128) {
-            umma_softmax<G, kNorm>(a, sums, u, tmem, n);
+            umma_softmax<D, G, kNorm>(a, sums, u, tmem, n);
         } else if (tid < 160) {
-            umma_sums<G>(u, tmem);
+            umma_sums<D, G>(u, tmem);
             tc::named_barrier_sync(5, 192);
             tc::tc_fence_after_sync();
             tc::tmem_dealloc(tmem, kTmemCols);
         } else if (tid < 192) {
-            umma_logits<G>(u, tmem, tc::smem_u32(dyn_tc + L::oQ));
+            umma_logits<D, G>(u, tmem, tc::smem_u32(dyn_tc + L::oQ));
             tc::named_barrier_arrive(5, 192);
         } else {
-            umma_load(u, (tid >> 5) & 1);
+            umma_load<D>(u, (tid >> 5) & 1);
         }
     } else {
         cache_part<D, G, kNorm, R>(a, sums, dyn_tc, in, n);

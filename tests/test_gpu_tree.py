@@ -121,13 +121,14 @@ def test_long_cache(dtype):
     check(call(x, dtype), reference(x), dtype)
 
 
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G,norm", [(1, False), (1, True), (2, False), (2, True)])
 @pytest.mark.parametrize("T,cluster", [(33, 8), (64, 4), (49, 2)])
-def test_full_trees_over_long_caches(G, norm, T, cluster):
+def test_full_trees_over_long_caches(d, G, norm, T, cluster):
     """33 to 64 nodes: several turns of the ring, every number of tiles modulo its places, one to eight CTAs' shares."""
     B, H = {8: (1, 9), 4: (3, 10), 2: (6, 10)}[cluster]
     lengths = [1800, 0, 1, 63, 64, 65, 640, 704, 768, 832, 896, 960, 1024, 1088, 1151, 1153, 1799, 17, 700]
-    x = make(T + G, B, H, T, 128, lengths, 1800, "bf16", route="all", unit=not norm)
+    x = make(T + G, B, H, T, d, lengths, 1800, "bf16", route="all", unit=not norm)
     check(call(x, "bf16", G=G, norm=norm), reference(x, G, norm), "bf16")
 
 
@@ -161,12 +162,12 @@ def test_ragged_trees(dtype, nodes):
     check(call(x, dtype), reference(x), dtype)
 
 
-@pytest.mark.parametrize("dtype,G", [("f32", 1), ("bf16", 1), ("bf16", 2)])
+@pytest.mark.parametrize("dtype,G,d", [("f32", 1, 128), ("bf16", 1, 128), ("bf16", 2, 128), ("bf16", 1, 64), ("bf16", 2, 64)])
 @pytest.mark.parametrize("T", [12, 40])
-def test_nothing_leaks(dtype, G, T):
+def test_nothing_leaks(dtype, G, d, T):
     """NaN and infinities in what a node does not see -- cache rows behind the length, nodes off its path, V of nodes that are
     not retained and K of its softmax -- reach no output."""
-    x = make(4, 2, 2, T, 128, [0, 5, 66, 190], 200, dtype, route="mixed", tree="random")
+    x = make(4, 2, 2, T, d, [0, 5, 66, 190], 200, dtype, route="mixed", tree="random")
     for b in range(2):
         for h in range(2):
             x["k_cache"][b, h, x["cache_len"][b, h]:] = np.nan
@@ -239,8 +240,8 @@ def test_what_is_not_a_tree_is_reported(dtype):
 
 def test_logits_that_grow_along_the_cache():
     """Every tile raises the running maximum by more than the sums' slack, so that all sums are rescaled again and again."""
-    for T, G in ((9, 1), (40, 1), (40, 2)):
-        x = make(T, 1, 2, T, 128, [900, 641], 900, "bf16", unit=True)
+    for T, G, d in ((9, 1, 128), (40, 1, 128), (40, 2, 128), (9, 1, 64), (40, 1, 64), (40, 2, 64)):
+        x = make(T, 1, 2, T, d, [900, 641], 900, "bf16", unit=True)
         # keys along the first nodes' mean direction, longer from tile to tile: logits grow to about 100
         x["q"][:] = x["q"][:, :1]
         ramp = np.linspace(0.0, 8.0, 900)[:, None]
