@@ -356,9 +356,12 @@ size_t tree_workspace_bytes() { return 256; }
 
 cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool tensor_cores, cudaStream_t st) {
     const int BH = s.B * s.H;
-    // CTAs per pair: as many as one resident set (one CTA per multiprocessor beyond 32 nodes, else two) has for each; with four
-    // softmax heads of 32 columns four at least, so that a CTA's columns belong to one of them
-    const int resident = s.L > 32 ? 148 : 2 * 148, cluster = BH * 8LL <= resident ? 8 : BH * 4LL <= resident || hg.G == 4 ? 4 : 2;
+    // CTAs per pair: as many as can be resident for all pairs at once.  A cluster lies within one of the GPU's groups of 16 to 18
+    // multiprocessors, so 148 of them hold 15 clusters of eight or 33 of four, twice that where a multiprocessor holds two CTAs
+    // (up to 32 nodes).  Pairs over 1638 keys of 128 columns, eight / four: 64 nodes of 16 pairs 31 / 19 us, of 8 17 / 18.5; 16
+    // nodes of 28 pairs 11.3 / 12.3, 32 of 32 17.9 / 16.0; four / two: 64 nodes of 33 pairs 20 / 25, of 48 37 / 26; 16 nodes of
+    // 60 15 / 17, of 71 17.1 / 17.3.  With four softmax heads of 32 columns four at least: a CTA's columns belong to one of them.
+    const int per = s.L > 32 ? 1 : 2, cluster = BH <= 14 * per ? 8 : BH <= 33 * per || hg.G == 4 ? 4 : 2;
     const Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
                  c.out, c.u, c.lse, (int32_t *)c.ws, s.H, s.L, c.cap, hg.G, cluster, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
     if (tensor_cores && hg.G <= 2) return launch_tree_tc(a, BH, s.d, st);
