@@ -474,10 +474,12 @@ evict_kernel(uint8_t *k_cache, uint8_t *v_cache, float *weight, int32_t *cache_l
 template <int kRowBytes>
 cudaError_t launch_evict(void *k_cache, void *v_cache, float *weight, int32_t *cache_len, int cap, int keep, int first, int recent,
                          int32_t *kept, int BH, cudaStream_t st) {
-    // Few pairs: a cluster for each, two CTAs per multiprocessor (with 192 KB of rows, one, the sixteenth cluster of eight waits
-    // for another's end); many: four.
-    int cluster = 1;
-    while (cluster < 8 && BH * cluster * 2 <= sm_count()) cluster *= 2;
+    // Few pairs: a cluster for each, as large as can be resident for all of them with two CTAs per multiprocessor (with 192 KB of
+    // rows, one, the sixteenth cluster of eight waits for another's end) and as leaves a CTA some 400 entries; many: four CTAs
+    // per multiprocessor.  Half of 8192 entries dropped, cluster / half as many: 48 pairs 55 / 73 us, 100 pairs 104 / 167; of
+    // 1638 entries 20 pairs (eight / four) 22 / 16, 48 (four / two) 20 / 20, 100 (two / one) 27 / 31.
+    int cluster = BH <= 28 ? 8 : BH <= 66 ? 4 : BH <= 148 ? 2 : 1;
+    while (cluster > 1 && cap < 400 * cluster) cluster /= 2;
     const int rows = (cluster > 1 ? 104 : 48) * 1024 / (2 * kRowBytes + 8), bytes = rows * (2 * kRowBytes + 8);
     auto kernel = cap <= 2048 * cluster ? evict_kernel<kRowBytes, 4> : evict_kernel<kRowBytes, 16>;
     cudaError_t e = allow_smem(kernel, 104 * 1024);

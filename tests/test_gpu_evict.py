@@ -159,7 +159,7 @@ def test_eviction(dtype, d, keep, first, recent):
     evict(k, v, w, n, keep, first, recent, dtype)
 
 
-@pytest.mark.parametrize("B,H", [(1, 1), (1, 2), (2, 8), (5, 8), (13, 13)])
+@pytest.mark.parametrize("B,H", [(1, 1), (1, 2), (2, 8), (5, 8), (5, 20), (13, 13)])
 def test_eviction_by_number_of_pairs(B, H):
     """Few pairs are moved by several CTAs each."""
     rng, k, v, w = cache(B, B, H, 2300, 64, "bf16")
@@ -190,7 +190,7 @@ def test_eviction_of_the_tail(B):
     evict(k, v, w, np.full((B, 4), 500, np.int32), 320, 320, 0, "bf16")
 
 
-@pytest.mark.parametrize("H", [2, 160])
+@pytest.mark.parametrize("H", [2, 90, 160])
 def test_eviction_of_long_caches(H):
     """More entries than a CTA holds in registers."""
     rng, k, v, w = cache(6, 1, H, 9001, 64, "bf16")
