@@ -2,11 +2,11 @@
 // tree_simt.cu's.
 //
 // A CTA has two parts that work side by side and meet at the end.  Some warps read the CTA's share of the cache, in tiles of 64
-// keys.  Up to 32 nodes (and with 64 columns) they are half of the warps and use warp-level MMAs: a tree has few query rows
+// keys.  Up to 32 nodes they are half of the warps and use warp-level MMAs: a tree has few query rows
 // for a tcgen05 tile of 128, and the call is bound by reading K/V once.  K and V pass in turns through a ring of asynchronous
 // copies; the warps share the tile by keys (and, beyond 16 nodes, by two groups of 16), each with its own running maximum and
 // sum, so that a key's row leaves shared memory once (twice) whatever the number of nodes, and their results meet at the
-// end.  Beyond 32 nodes of 128 columns that arithmetic takes twice the time of the bytes, and tcgen05 takes it over (below).
+// end.  Beyond 32 nodes that arithmetic takes twice the time of the bytes, and tcgen05 takes it over (below).
 // A running maximum moves only when a logit exceeds it by 2^8.  Probabilities meet V rounded to bf16 (2^-8 of themselves, V's
 // own precision); their sum is taken before the rounding.
 //
@@ -19,7 +19,7 @@
 //
 // B200: one token of 64 x 16 heads over 1638 keys 155 us (930 MB: 6.0 TB/s, 92 % of a copy's rate); 32 nodes 216 us (4.5 TB/s:
 // of a CTA's 53000 cycles the last 10000 are the join, which no load overlaps but the neighbour CTA's); 64 nodes of 8 x 16
-// heads over up to 6554 keys 92 us (161 us with warp-level MMAs); 16 nodes of 16 heads 11 us.
+// heads over up to 6554 keys 92 us (161 us with warp-level MMAs; with 64 columns 67 and 106); 16 nodes of 16 heads 11 us.
 #include <algorithm>
 #include "tree_common.cuh"
 
@@ -56,9 +56,9 @@ template <int D, int R> struct Layout {
     using S = Sums<2, kRows>;
     using N = Nodes<2, kRows>;
     // Two CTAs of 8 warps per multiprocessor, or one of 16: half of a CTA's warps read the cache, each 16 rows and a share of the
-    // tile's keys.  Beyond 32 nodes of 128 columns the cache's products are tcgen05 MMAs: four warps of softmax and four that issue
+    // tile's keys.  Beyond 32 nodes the cache's products are tcgen05 MMAs: four warps of softmax and four that issue
     // the copies of K and V and the two products, beside eight for the tree's own part.  (The same for 17 to 32 nodes, with one
-    // softmax warp a CTA: 224 us where warp-level MMAs take 216.)
+    // softmax warp a CTA: 224 us for 64 x 16 heads over 1638 keys, where warp-level MMAs take 216.)
     static constexpr bool kUmma = R == 4;
     static constexpr int kCtas = R == 4 ? 1 : 2, kWarps = R == 4 ? 8 : 4;      // kWarps: of the tree's part
     static constexpr int kHalf = 32 * kWarps, kReaders = kUmma ? 256 : kHalf, kThreads = kReaders + kHalf;
@@ -335,7 +335,7 @@ __device__ void cache_part(const Args &a, typename Layout<D, R>::S *sums, uint8_
 }
 
 // ------------------------------------------------------------------------------------------
-// The CTA's share of the cache with tcgen05 (33 to 64 nodes, 128 columns).  An MMA has 128 rows: the even tiles' logits use rows
+// The CTA's share of the cache with tcgen05 (33 to 64 nodes).  An MMA has 128 rows: the even tiles' logits use rows
 // 0 .. 63 of it, the odd ones' 64 .. 127 -- the operand is q behind, or ahead of, whatever shared memory holds there, and what the
 // other rows get is never looked at -- so that all four warps have a row per thread and tiles of their own, two key groups with a
 // running maximum each.  Probabilities take the logits' place in tensor memory as the second product's operand.  Per tile the
@@ -1009,7 +1009,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant_
     const int bh = blockIdx.x / a.cluster, rank = blockIdx.x - bh * a.cluster, b = bh / a.H, h = bh - b * a.H, tid = threadIdx.x;
     if (L::kUmma && tid == 128) {
         umma_init(&bars, kNorm, wait_kcycles);
-        if (a.cap > 0) { tc::prefetch_tmap(&map_k); tc::prefetch_tmap(&map_v); }
+        tc::prefetch_tmap(&map_k);
+        tc::prefetch_tmap(&map_v);
     }
     tc::grid_dependency_wait();
     if (L::kUmma && tid / 32 == 4) tc::tmem_alloc(&bars.tmem, kTmemCols);
@@ -1087,8 +1088,8 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
     cudaError_t e = allow_smem(kernel, Layout<D, R>::kTotal);
     if (e != cudaSuccess) return e;
     CUtensorMap map_k = {}, map_v = {};
-    if (Layout<D, R>::kUmma && a.cap > 0 && (!tch::make_map_2d(&map_k, a.k_cache, (uint64_t)BH * a.cap, D, kTileKeys) ||
-                                             !tch::make_map_2d(&map_v, a.v_cache, (uint64_t)BH * a.cap, D, kTileKeys)))
+    if (Layout<D, R>::kUmma && (!tch::make_map_2d(&map_k, a.k_cache, (uint64_t)BH * a.cap, D, kTileKeys) ||
+                                !tch::make_map_2d(&map_v, a.v_cache, (uint64_t)BH * a.cap, D, kTileKeys)))
         return cudaErrorInvalidValue;
     return launch_clusters(kernel, BH * a.cluster, a.cluster, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st, map_k, map_v, a,
                            debug_wait_kcycles());
