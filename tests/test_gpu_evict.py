@@ -318,6 +318,44 @@ def test_calls_one_behind_the_other(dtype, T):
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
 
 
+@pytest.mark.parametrize("dtype,T", [("f32", 9), ("bf16", 9), ("bf16", 40)])
+def test_captured_and_on_another_stream(dtype, T):
+    """Weights and eviction in a CUDA graph, replayed on new contents on a stream of its own, against the calls themselves."""
+    from paper_2602_03681_b200 import binding
+    B, H, d, cap, keep = 2, 4, 128, 900, 200
+    x = case(9, B, H, T, d, [0, 150, 200, 201, 900, 899, 512, 640], cap, dtype)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    la, sm = scales(d, 1, False)
+    q, kc, vc = dev(x["q"], dt), dev(x["k_cache"], dt), dev(x["v_cache"], dt)
+    lse, visible, weight, n = dev(x["lse"][:, :, 0]), dev(x["visible"]), dev(x["weight"]), dev(x["cache_len"])
+    kept = torch.zeros(B, H, keep, dtype=torch.int32, device="cuda")
+    p = binding.make_params(B, H, T, d, binding._dtype_code(q), la, sm)
+    start = [y.clone() for y in (kc, vc, weight, n, kept)]
+
+    def run():
+        binding.natsl_cache_weights(q, lse, visible, kc, n, weight, p)
+        binding.natsl_cache_evict(kc, vc, weight, n, keep, 4, 30, kept, p)
+
+    def reset():
+        for y, s0 in zip((kc, vc, weight, n, kept), start):
+            y.copy_(s0)
+        torch.cuda.synchronize()
+
+    run()
+    torch.cuda.synchronize()
+    want = [y.clone() for y in (kc, vc, weight, n, kept)]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    reset()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for _ in range(3):
+        reset()
+        with torch.cuda.stream(side):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, w) for y, w in zip((kc, vc, weight, n, kept), want))
+
+
 @pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 40), ("f32", 9)])
 def test_offsets_past_32_bits(dtype, T):
     """Caches of more than 2^31 elements a pair: the second pair's lies behind them.  All four calls give what they give for
