@@ -115,10 +115,9 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             }
             __syncwarp();
         }
-        if (!ok) {                                // no copy in flight when the CTA retires
-            if (q > 0) mbar_wait_drain(&bar.q_full, (q - 1) & 1);
-            for (int e = max(0, i - kStages); e < i; ++e) mbar_wait_drain(&bar.full[e % kStages], (e / kStages) & 1);
-        }
+        // no copy in flight when the CTA retires, whoever has given up
+        if (q > 0) mbar_wait_drain(&bar.q_full, (q - 1) & 1);
+        for (int e = max(0, i - kStages); e < i; ++e) mbar_wait_drain(&bar.full[e % kStages], (e / kStages) & 1);
     } else if (tid >= kWorkers) {                 // ---- products ----
         constexpr uint32_t idesc = make_idesc(kFmtBF16, kKeys, kRows, false, false);
         const int nt = (int)uniform((uint32_t)tiles), all = nt * (int)uniform((uint32_t)chunks);
@@ -148,13 +147,11 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
             }
             if (++t == nt) { t = 0; ++q; }
         }
-        if (!ok) {                                // no MMA in flight when tensor memory goes
-            if (elect_one()) {
-                mma_commit(&bar.drain);
-                mbar_wait_drain(&bar.drain, 0);
-            }
-            __syncwarp();
+        if (elect_one()) {                        // no MMA in flight when tensor memory goes
+            mma_commit(&bar.drain);
+            mbar_wait_drain(&bar.drain, 0);
         }
+        __syncwarp();
     } else {                                      // ---- the sums ----
         const int g = warp >> 2, r = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;

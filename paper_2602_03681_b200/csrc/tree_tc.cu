@@ -402,11 +402,11 @@ template <int D> __device__ void umma_load(const UmmaShare<D> &in, int kv) {
         }
         __syncwarp();
     }
-    if (t < tiles)                                // no copy in flight when the CTA retires
-        for (int i = max(0, t - stages); i < t; ++i) mbar_wait_drain(&bar->full[kv][in.stage(kv, i)], in.phase(kv, i));
+    // no copy in flight when the CTA retires, whoever has given up
+    for (int i = max(0, t - stages); i < t; ++i) mbar_wait_drain(&bar->full[kv][in.stage(kv, i)], in.phase(kv, i));
 }
 
-__device__ __forceinline__ void umma_drain(uint64_t *bar) {              // no MMA in flight when the CTA retires
+__device__ __forceinline__ void umma_drain(uint64_t *bar) {              // nor an MMA
     if (tc::elect_one()) {
         tc::mma_commit(bar);
         tc::mbar_wait_drain(bar, 0);
@@ -442,7 +442,7 @@ __device__ void umma_logits(const UmmaShare<D> &in, uint32_t tmem, uint32_t q_at
         }
         __syncwarp();
     }
-    if (!ok) umma_drain(&bar->drain[0]);
+    umma_drain(&bar->drain[0]);
 }
 
 // The group's sums += probabilities V.
@@ -473,7 +473,7 @@ __device__ void umma_sums(const UmmaShare<D> &in, uint32_t tmem) {
         }
         __syncwarp();
     }
-    if (!ok) umma_drain(&bar->drain[1]);
+    umma_drain(&bar->drain[1]);
 }
 
 // The four softmax warps: thread = row of a key group.
