@@ -1013,7 +1013,10 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant_
         tc::prefetch_tmap(&map_v);
     }
     tc::grid_dependency_wait();
-    if (L::kUmma && tid / 32 == 4) tc::tmem_alloc(&bars.tmem, kTmemCols);
+    if (L::kUmma && tid / 32 == 4) {
+        __syncwarp();                             // (one lane comes from the branch above; an allocation is the whole warp's)
+        tc::tmem_alloc(&bars.tmem, kTmemCols);
+    }
     const NodeRow node = load_node(a, b, h, tid >= kReaders ? tid - kReaders : a.T);
     const int n = nodes_of(a, b), cols = D / a.cluster;
     const Share share = share_of(a.cache_len[bh], a.cap, a.cluster, rank);

@@ -124,3 +124,40 @@ def test_the_rules_find_what_they_are_for():
     assert not barriers_behind_a_wait(ok + "if (ok) { x(); } __syncthreads();")
     assert not barriers_behind_a_wait("for (;;) { if (p) { if (!mbar_wait(&a, 0, f)) continue; } else { __syncthreads(); } }")
     assert not barriers_behind_a_wait("for (;;) { for (;;) { if (!mbar_wait(&a, 0, f)) break; } __syncthreads(); }")
+
+
+def allocates_with_a_warp_apart(body, constants=""):
+    """Whether a warp may come to an allocation of tensor memory (an .aligned instruction: the whole warp at once) straight
+    from a branch that one of its lanes took, with nothing between that brings the lanes together again."""
+    at = body.find("tmem_alloc(")
+    if at < 0:
+        return False
+    warp = re.findall(r"(?:\bwarp|\btid\s*/\s*32)\s*==\s*(\w+)", body[:at])[-1]
+    while not warp.isdigit():
+        m = re.search(r"\b%s\s*=\s*(\w+)" % warp, constants)
+        if not m:
+            break
+        warp = m.group(1)
+    for m in re.finditer(r"\btid\s*==\s*(\d+)|\belect_one\(\)|\blane\s*==\s*0", body[:at]):
+        if m.group(1) and warp.isdigit() and int(m.group(1)) // 32 != int(warp):
+            continue                                          # (another warp's lane)
+        if not re.search(r"__syncwarp\(\)|" + BARRIER.pattern, body[m.end():at]):
+            return True
+    return False
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_warps_allocate_tensor_memory_together(source):
+    with open(os.path.join(CSRC, source)) as f:
+        constants = f.read()
+    for name, body in kernels(os.path.join(CSRC, source)):
+        assert not allocates_with_a_warp_apart(body, constants), name
+
+
+def test_the_rule_on_allocations_finds_what_it_is_for():
+    assert allocates_with_a_warp_apart("if (tid == 128) { x(); } if (tid / 32 == 4) tc::tmem_alloc(&b, 512);")
+    assert allocates_with_a_warp_apart("if (warp == kW) { if (elect_one()) { x(); } tmem_alloc(&b, 64); }", "kW = 8;")
+    assert not allocates_with_a_warp_apart("if (tid == 128) { x(); } if (tid / 32 == 4) { __syncwarp(); tc::tmem_alloc(&b, 512); }")
+    assert not allocates_with_a_warp_apart("if (warp == kW) { if (elect_one()) { x(); } __syncwarp(); tmem_alloc(&b, 64); }", "kW = 8;")
+    assert not allocates_with_a_warp_apart("if (tid == 0) { x(); } if (warp == kW) tmem_alloc(&b, 64);", "constexpr int kW = 4;")
+    assert not allocates_with_a_warp_apart("x();")
