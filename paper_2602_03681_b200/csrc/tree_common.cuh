@@ -51,9 +51,9 @@ template <int kHeads, int kRows> struct Sums {
 template <int kHeads, int kRows> struct Nodes {
     unsigned long long above[kRows];              // strict ancestors
     unsigned long long fold, keep;                // nodes that update the state; nodes whose K/V count as retained
-    float2 total[kRows];                          // sum of g from the context up to and with the node, as two fp32 terms, -inf
-    int wipes[kRows];                             // left out and counted here
-    float whole[kRows], beta[kRows], g[kRows];    // whole: exp of that sum
+    float2 total[kRows];                          // sum of g from the context up to and with the node, as two fp32 terms; a g whose
+    int wipes[kRows];                             // exp is zero is left out and counted here
+    float whole[kRows], beta[kRows], g[kRows];    // whole: exp of that sum; g: -inf where its exp is zero
     float rq_la[kRows], rk_la[kRows];             // L2 factors; RMS factors per softmax head
     float rq_sm[kHeads][kRows], rk_sm[kHeads][kRows];
     int parent[kRows];
@@ -82,7 +82,9 @@ __device__ __forceinline__ void walk_nodes(const Args &a, int b, int h, int n, i
         if (tid < kRows) {
             nd->parent[tid] = par;
             nd->beta[tid] = tid < n ? row.beta : 0.f;
-            nd->g[tid] = row.g;
+            // A decay that is zero in fp32 (g below -104) ends what comes from above, as one of -inf does: left in the sums, a large
+            // enough g would take the others' bits with it.  So they are sums of at most 64 values above -104.
+            nd->g[tid] = expf(row.g) == 0.f ? -INFINITY : row.g;
         }
         const unsigned f = __ballot_sync(0xffffffffu, tid < n && row.route != 1), k = __ballot_sync(0xffffffffu, tid < n && row.route != 0);
         if ((tid & 31) == 0) {
@@ -114,7 +116,7 @@ __device__ __forceinline__ void walk_nodes(const Args &a, int b, int h, int n, i
         nd->whole[tid] = wipes || tid >= n ? 0.f : expf(hi);
     }
 }
-// Decay on the path from its node j (exclusive) to i, and zero as soon as a g of -inf lies on it.
+// Decay on the path from its node j (exclusive) to i, and zero as soon as a zero one lies on it.
 __device__ __forceinline__ float decay_between(float2 total_i, int wipes_i, float2 total_j, int wipes_j) {
     const float x = expf((total_i.x - total_j.x) + (total_i.y - total_j.y));
     return wipes_i != wipes_j ? 0.f : x;

@@ -427,3 +427,36 @@ def test_beside_other_users_of_tensor_memory():
     assert all(torch.equal(t[m], y) for m, y in zip(("out", "u"), want))
     assert torch.equal(weight, once) and torch.equal(out, fwd)
     assert binding.natsl_device_status(t["ws"]) == 0 and binding.natsl_device_status(wf) == 0
+
+
+@pytest.mark.parametrize("dtype,T", [("f32", 12), ("bf16", 12), ("bf16", 40)])
+@pytest.mark.parametrize("g", [-95.0, -200.0, -1e9, -1e30, float(np.finfo(np.float32).min)])
+@pytest.mark.parametrize("times", [1, 2])
+def test_decays_that_are_zero_in_fp32(dtype, T, g, times):
+    """A finite g whose decay is zero in fp32 (a masked gate, say), once and twice on a path: what comes behind it decays by its own
+    g, as in natsl_decode_step, which multiplies the state by exp(g) token by token."""
+    x = make(16, 1, 2, T, 64, [40, 0], 40, dtype, route="all", tree="chain")
+    x["g"][:, [3, 6][:times]] = g
+    check(call(x, dtype), reference(x), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_decay_to_nothing_and_generation(dtype):
+    """The same through natsl_decode_step: the step's outputs and the committed state."""
+    from paper_2602_03681_b200 import binding
+    H, T, d = 2, 9, 64
+    x = make(17, 1, H, T, d, [20, 0], 40, dtype, route=0, tree="chain")
+    x["g"][:, 2], x["g"][:, 5] = -1e30, np.finfo(np.float32).min
+    x["path"][0], x["n_path"][0] = np.arange(T), T
+    t = call(x, dtype)
+    commit(t, x)
+    ref = upload(x, dtype)
+    la, sm = scales(d, 1, False)
+    for i in range(T):
+        row = {m: ref[m][:, i].contiguous() for m in ("q", "k", "v", "g", "beta", "route", "w")}
+        p = binding.make_params(1, H, 0, d, binding._dtype_code(row["q"]), la, sm, w=row["w"])
+        out = torch.empty_like(row["q"])
+        binding.natsl_decode_step(row["q"], row["k"], row["v"], row["g"], row["beta"], row["route"], ref["state"], ref["k_cache"],
+                                  ref["v_cache"], ref["cache_len"], out, p, binding.alloc_workspace(p, binding.OP_DECODE))
+        check_stored(t["out"][0, i].float().cpu().numpy(), out[0].double().cpu().numpy(), TOL[dtype], dtype, large_only=False)
+    assert rel_err(t["state"].cpu().numpy(), ref["state"].cpu().numpy()) <= 1e-4
