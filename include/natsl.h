@@ -376,8 +376,8 @@ int natsl_tree_step(const void *q, const void *k, const void *v, const float *g,
  *   path [B,L] i32: the accepted nodes from the context on, each the parent of the next (so strictly
  *       ascending), n_path [B] i32 of them (0: nothing is accepted); the rest of path is not read;
  *   state [B,H,d,d] fp32, k_cache,v_cache [B,H,cache_cap,d], cache_len [B,H] i32: updated in place.
- * A (sequence, head) whose cache has no room for its retained tokens is left untouched and reported as
- * NATSL_ERR_CACHE_FULL; a sequence whose path is not strictly ascending inside [0, L), or whose n_path lies
+ * A (sequence, head) whose cache has no room for its retained tokens, or whose length lies outside
+ * [0, cache_cap], is left untouched and reported as NATSL_ERR_CACHE_FULL; a sequence whose path is not strictly ascending inside [0, L), or whose n_path lies
  * outside [0, L], is left untouched and reported as NATSL_ERR_TREE.  ws: the tree's workspace (for the status
  * word).  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, CUDA.
  */

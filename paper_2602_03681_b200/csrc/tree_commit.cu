@@ -91,9 +91,10 @@ tree_commit_kernel(const ST *__restrict__ k, const ST *__restrict__ v, const flo
     const int kept = __popcll(s_keep);
     if (tid == 0) {
         if (bad) atomicMin(status, (int)NATSL_ERR_TREE);
-        if (n_raw != n_old || (!bad && n_old + kept > cap)) atomicMin(status, (int)NATSL_ERR_CACHE_FULL);
+        if (n_raw != n_old || (!bad && kept > cap - n_old)) atomicMin(status, (int)NATSL_ERR_CACHE_FULL);
     }
-    if (bad || kept > cap - n_old) return;        // (the same for the whole CTA) the pair is left untouched
+    // (the same for the whole CTA) What is reported is left untouched, so that the caller can mend it and commit again.
+    if (bad || n_raw != n_old || kept > cap - n_old) return;
     if (m == 0) return;
     if (tid < m) {
         float x = 1.f;

@@ -460,3 +460,32 @@ def test_decay_to_nothing_and_generation(dtype):
                                   ref["v_cache"], ref["cache_len"], out, p, binding.alloc_workspace(p, binding.OP_DECODE))
         check_stored(t["out"][0, i].float().cpu().numpy(), out[0].double().cpu().numpy(), TOL[dtype], dtype, large_only=False)
     assert rel_err(t["state"].cpu().numpy(), ref["state"].cpu().numpy()) <= 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [-5, -2 ** 31, 17, 2 ** 31 - 1])
+@pytest.mark.parametrize("route", [0, "mixed"])
+def test_commit_to_a_length_out_of_range(dtype, length, route):
+    """Reported, and nothing of the pair is written, whether or not its path retains a token: with the length put right the
+    same commit does what it always does."""
+    from paper_2602_03681_b200 import binding
+    x = make(5, 2, 2, 8, 64, [3, 5, 0, 7], 16, dtype, tree="chain", route=route)
+    x["path"][:], x["n_path"][:] = np.arange(8), 5
+    t = call(x, dtype)
+    right = t["cache_len"].clone()
+    t["cache_len"][1, 0] = length
+    before = [t[m][1, 0].clone() for m in ("state", "k_cache", "v_cache", "cache_len")]
+    commit(t, x)
+    assert binding.natsl_device_status(t["ws"]) == binding.ERR_CACHE_FULL
+    assert all(torch.equal(t[m][1, 0], y) for m, y in zip(("state", "k_cache", "v_cache", "cache_len"), before))
+    one = {m: t[m][1:, :1].contiguous() for m in ("state", "k_cache", "v_cache")}
+    one["cache_len"] = right[1:, :1].contiguous()
+    for m in ("k", "v", "g", "route", "u"):
+        one[m] = t[m][1:, :, :1].contiguous()
+    one["path"], one["n_path"] = t["path"][1:].contiguous(), t["n_path"][1:].contiguous()
+    one["p"] = binding.make_params(1, 1, 8, 64, binding._dtype_code(t["k"]), 1.0, 1.0)
+    one["ws"] = t["ws"]
+    commit(one, x)
+    for m in ("state", "k_cache", "v_cache", "cache_len"):
+        t[m][1:, :1] = one[m]
+    check_commit(t, x)
