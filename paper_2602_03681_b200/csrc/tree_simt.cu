@@ -51,7 +51,7 @@ __device__ void cache_part(const Args &a, SimtSums *sums, float *out_acc, float 
     float *sq = sm, *sk = sq + TT * P, *sv = sk + kKeys * P, *sp = sv + kKeys * D, *s_m = sp + G * TT * kKeys,
           *s_z = s_m + G * TT, *s_f = s_z + G * TT, *s_rq = s_f + G * TT, *s_rk = s_rq + G * TT;
     const bool norm = a.norm_eps >= 0.f;
-    const float scale = a.scale_sm * kLog2e;      // (logits in base-2 units: on q)
+    const float to_base2 = a.scale_sm * kLog2e, scale = norm ? 1.f : to_base2;      // (on q, or on q's factors)
 #pragma unroll 4
     for (int i = tid; i < TT * D / 4; i += kHalf) {
         const int t = i / (D / 4), x = (i - t * (D / 4)) * 4;
@@ -68,10 +68,10 @@ __device__ void cache_part(const Args &a, SimtSums *sums, float *out_acc, float 
         }
         return s;
     };
-    if (norm) {                                   // (q is scaled already: its mean square by the scale's)
+    if (norm) {
         sync();
         for (int i = tid; i < G * TT; i += kHalf)
-            s_rq[i] = rsqrtf(factor(sq + i % TT * P + i / TT * ds) / (ds * scale * scale) + a.norm_eps);
+            s_rq[i] = to_base2 * rsqrtf(factor(sq + i % TT * P + i / TT * ds) / ds + a.norm_eps);
     }
     const int col = tid % D, r0 = tid / D * RC, gc = col / ds;
     float acc[RC];

@@ -489,3 +489,14 @@ def test_commit_to_a_length_out_of_range(dtype, length, route):
     for m in ("state", "k_cache", "v_cache", "cache_len"):
         t[m][1:, :1] = one[m]
     check_commit(t, x)
+
+
+@pytest.mark.parametrize("dtype,G,norm,T", [("f32", 1, True, 6), ("f32", 4, True, 6), ("bf16", 4, True, 6), ("bf16", 2, True, 6),
+                                            ("bf16", 2, True, 40), ("f32", 1, False, 6), ("bf16", 1, False, 40)])
+@pytest.mark.parametrize("sm", [0.0, 1e-23, -0.3])
+def test_any_logit_scale(dtype, G, norm, T, sm, monkeypatch):
+    """Zero (every visible key counts the same), one whose square is zero, and a negative one."""
+    import test_gpu_tree
+    monkeypatch.setattr(test_gpu_tree, "scales", lambda d, G, norm: (d ** -0.5, sm))
+    x = make(3, 1, 2, T, 128, [50, 3], 50, dtype, route="all", unit=not norm)
+    check(call(x, dtype, G=G, norm=norm), reference(x, G, norm), dtype)
