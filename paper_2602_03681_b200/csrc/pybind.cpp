@@ -1,14 +1,18 @@
 // Python entry points of the calls a program makes per token, layer or step: the same names and argument
 // order as binding.py's, marshalled natively.  A generation step is a 7-12 us kernel; marshalling its
 // twelve tensors through ctypes and asking torch for the current stream in Python took 13-16 us per call and
-// set the pace of small batches.  Here a tensor argument is checked (device-resident, contiguous),
+// set the pace of small batches.  Here a tensor argument is checked (device-resident, contiguous; in the calls of
+// speculative generation and of a bounded cache, whose tensors share dimensions, large enough too: NATSL_ERR_SHAPE),
 // unwrapped and passed on without an intermediate Python object.
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cstdint>
 #include <exception>
+#include <initializer_list>
 
 #include "../../include/natsl.h"
 
@@ -68,6 +72,50 @@ struct Args {
         }
         PyBuffer_Release(&b);                // (the caller's argument keeps the structure alive)
         return ok ? static_cast<const natsl_params *>(p) : nullptr;
+    }
+};
+
+// The tensors of a call against its parameters: whether each has room for what the call reads or writes of it, and whether
+// those that share a capacity agree on it.  The C call sees addresses alone and would run past their ends.  What is None, or no
+// tensor at all, is somebody else's to judge, and so are parameters that the call refuses itself.
+struct Room {
+    PyObject *const *v;
+    const natsl_params *p;
+    const size_t esz = p->dtype == NATSL_BF16 ? 2 : 4;
+    bool ok = true;
+
+    const at::Tensor *at(int i) const { return THPVariable_Check(v[i]) ? &THPVariable_Unpack(v[i]) : nullptr; }
+    Room &has(int i, size_t size, std::initializer_list<int64_t> dims) {
+        const at::Tensor *t = at(i);
+        double bytes = (double)size;          // (exact up to 2^53; a tensor is far smaller)
+        for (int64_t n : dims) bytes *= (double)std::max<int64_t>(n, 0);
+        ok = ok && (!t || (double)t->numel() * (double)t->element_size() >= bytes);
+        return *this;
+    }
+    Room &tokens(std::initializer_list<int> list, size_t size) {                  // [B,L,H,d]
+        for (int i : list) has(i, size, {p->B, p->L, p->H, p->d});
+        return *this;
+    }
+    Room &heads(std::initializer_list<int> list, size_t size) {                   // [B,L,H]
+        for (int i : list) has(i, size, {p->B, p->L, p->H});
+        return *this;
+    }
+    int64_t capacity(int i) const {           // of a cache [B,H,cap,d]; -1: none, and nothing is held against it
+        const at::Tensor *t = at(i);
+        return t && t->dim() > 2 ? t->size(2) : -1;
+    }
+    Room &caches(std::initializer_list<int> list, int64_t cap) {
+        for (int i : list) {
+            const at::Tensor *t = at(i);
+            ok = ok && (!t || cap < 0 || (t->dim() == 4 && t->size(2) == cap && t->size(3) == p->d)) && cap <= INT32_MAX;
+            has(i, esz, {p->B, p->H, cap, p->d});
+        }
+        return *this;
+    }
+    Room &per_entry(int i, int64_t n) {       // [B,H,n] of four bytes
+        const at::Tensor *t = at(i);
+        ok = ok && (!t || n < 0 || (t->dim() > 0 && t->size(-1) == n));
+        return has(i, 4, {p->B, p->H, n});
     }
 };
 
@@ -177,6 +225,12 @@ PyObject *score_layer(PyObject *, PyObject *const *v, Py_ssize_t n) {
 PyObject *tree_step(PyObject *, PyObject *const *v, Py_ssize_t n) {
     if (!count_is(n, 16)) return nullptr;
     Args a{v};
+    const natsl_params *p = a.params(14);
+    if (!p) return nullptr;
+    Room r{v, p};
+    r.tokens({0, 1, 2, 12}, r.esz).tokens({13}, 4).heads({3, 4}, 4).heads({5}, 1).has(6, 4, {p->B, p->L}).has(7, 4, {p->B});
+    r.has(8, 4, {p->B, p->H, p->d, p->d}).caches({9, 10}, r.capacity(9)).has(11, 4, {p->B, p->H});
+    if (!r.ok) return PyLong_FromLong(NATSL_ERR_SHAPE);
     const void *q = a.ptr<void>(0), *k = a.ptr<void>(1), *vv = a.ptr<void>(2);
     const float *g = a.ptr<float>(3), *beta = a.ptr<float>(4);
     const uint8_t *route = a.ptr<uint8_t>(5);
@@ -187,7 +241,6 @@ PyObject *tree_step(PyObject *, PyObject *const *v, Py_ssize_t n) {
     const int32_t cap = (int32_t)a.size(9, 2);
     void *out = a.ptr<void>(12), *ws = a.ptr<void>(15);
     float *u = a.ptr<float>(13);
-    const natsl_params *p = a.params(14);
     const size_t wb = a.numel(15);
     NATSL_CALL(natsl_tree_step(q, k, vv, g, beta, route, parent, nodes, state, kc, vc, len, cap, out, u, p, ws, wb, st));
 }
@@ -195,6 +248,12 @@ PyObject *tree_step(PyObject *, PyObject *const *v, Py_ssize_t n) {
 PyObject *tree_commit(PyObject *, PyObject *const *v, Py_ssize_t n) {
     if (!count_is(n, 13)) return nullptr;
     Args a{v};
+    const natsl_params *p = a.params(11);
+    if (!p) return nullptr;
+    Room r{v, p};
+    r.tokens({0, 1}, r.esz).tokens({4}, 4).heads({2}, 4).heads({3}, 1).has(5, 4, {p->B, p->L}).has(6, 4, {p->B});
+    r.has(7, 4, {p->B, p->H, p->d, p->d}).caches({8, 9}, r.capacity(8)).has(10, 4, {p->B, p->H});
+    if (!r.ok) return PyLong_FromLong(NATSL_ERR_SHAPE);
     const void *k = a.ptr<void>(0), *vv = a.ptr<void>(1);
     const float *g = a.ptr<float>(2);
     const uint8_t *route = a.ptr<uint8_t>(3);
@@ -204,7 +263,6 @@ PyObject *tree_commit(PyObject *, PyObject *const *v, Py_ssize_t n) {
     void *kc = a.ptr<void>(8), *vc = a.ptr<void>(9), *ws = a.ptr<void>(12);
     int32_t *len = a.ptr<int32_t>(10);
     const int32_t cap = (int32_t)a.size(8, 2);
-    const natsl_params *p = a.params(11);
     const size_t wb = a.numel(12);
     NATSL_CALL(natsl_tree_commit(k, vv, g, route, u, path, n_path, state, kc, vc, len, cap, p, ws, wb, st));
 }
@@ -212,6 +270,12 @@ PyObject *tree_commit(PyObject *, PyObject *const *v, Py_ssize_t n) {
 PyObject *cache_weights(PyObject *, PyObject *const *v, Py_ssize_t n) {
     if (!count_is(n, 7)) return nullptr;
     Args a{v};
+    const natsl_params *p = a.params(6);
+    if (!p) return nullptr;
+    Room r{v, p};
+    r.tokens({0}, r.esz).heads({2}, 4).has(1, 4, {p->B, p->H, std::max(p->G, 1), p->L}).caches({3}, r.capacity(3));
+    r.has(4, 4, {p->B, p->H}).per_entry(5, r.capacity(3));
+    if (!r.ok) return PyLong_FromLong(NATSL_ERR_SHAPE);
     const void *q = a.ptr<void>(0);
     const float *lse = a.ptr<float>(1);
     const int32_t *visible = a.ptr<int32_t>(2);
@@ -219,20 +283,26 @@ PyObject *cache_weights(PyObject *, PyObject *const *v, Py_ssize_t n) {
     const int32_t *len = a.ptr<int32_t>(4);
     float *weight = a.ptr<float>(5);
     const int32_t cap = (int32_t)a.size(3, 2);
-    const natsl_params *p = a.params(6);
     NATSL_CALL(natsl_cache_weights(q, lse, visible, kc, len, cap, weight, p, st));
 }
 
 PyObject *cache_evict(PyObject *, PyObject *const *v, Py_ssize_t n) {
     if (!count_is(n, 9)) return nullptr;
     Args a{v};
+    const natsl_params *p = a.params(8);
+    if (!p) return nullptr;
+    const long keep_as = a.integer(4), first_as = a.integer(5), recent_as = a.integer(6);
+    if (!a.ok) return nullptr;
+    Room r{v, p};
+    r.caches({0, 1}, r.capacity(0)).per_entry(2, r.capacity(0)).has(3, 4, {p->B, p->H}).per_entry(7, keep_as);
+    for (long x : {keep_as, first_as, recent_as}) r.ok = r.ok && x >= 0 && x <= INT32_MAX;
+    if (!r.ok) return PyLong_FromLong(NATSL_ERR_SHAPE);
     void *kc = a.ptr<void>(0), *vc = a.ptr<void>(1);
     float *weight = a.ptr<float>(2);
     int32_t *len = a.ptr<int32_t>(3);
     const int32_t cap = (int32_t)a.size(0, 2);
-    const int32_t keep = (int32_t)a.integer(4), first = (int32_t)a.integer(5), recent = (int32_t)a.integer(6);
+    const int32_t keep = (int32_t)keep_as, first = (int32_t)first_as, recent = (int32_t)recent_as;
     int32_t *kept = a.ptr<int32_t>(7);
-    const natsl_params *p = a.params(8);
     NATSL_CALL(natsl_cache_evict(kc, vc, weight, len, cap, keep, first, recent, kept, p, st));
 }
 
