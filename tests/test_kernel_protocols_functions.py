@@ -1,0 +1,59 @@
+"""The rule of test_kernel_protocols.py in the functions that kernels are made of: whether a thread arrives at a barrier of many,
+the cluster's and the arrivals without a wait included, must not depend on how a bounded wait of its own ended."""
+import glob
+import os
+import re
+
+import pytest
+
+import test_kernel_protocols as protocols
+
+SOURCES = sorted(os.path.basename(p) for p in glob.glob(os.path.join(protocols.CSRC, "*.cu*")))
+BARRIER = re.compile(r"\b(named_barrier_sync|named_barrier_arrive|__syncthreads\w*|cluster_arrive|cluster_wait)\s*\(")
+
+
+def functions(path):
+    """[(name, body without comments)] of a source file's device functions."""
+    with open(path) as f:
+        text = f.read()
+    text = re.sub(r"//[^\n]*", "", re.sub(r"/\*.*?\*/", "", text, flags=re.S))
+    found = []
+    for m in re.finditer(r"__device__\b[^;{}()]*?\b(\w+)\s*\(", text):
+        at, depth = m.end(), 1
+        while depth:                                          # (behind the parameters)
+            depth += {"(": 1, ")": -1}.get(text[at], 0)
+            at += 1
+        rest = re.match(r"\s*(?:const\s*)?\{", text[at:])
+        if not rest:
+            continue                                          # (a declaration, a constructor's list)
+        at += rest.end()
+        depth, end = 1, at
+        while depth:
+            depth += {"{": 1, "}": -1}.get(text[end], 0)
+            end += 1
+        found.append((m.group(1), text[at:end - 1]))
+    return found
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_no_barrier_of_a_function_stands_behind_one_threads_wait(source, monkeypatch):
+    monkeypatch.setattr(protocols, "BARRIER", BARRIER)
+    for name, body in functions(os.path.join(protocols.CSRC, source)):
+        assert not protocols.barriers_behind_a_wait("{" + body + "}"), name      # (so that a return leaves something)
+
+
+def test_the_functions_are_found():
+    names = [n for n, _ in functions(os.path.join(protocols.CSRC, "tree_tc.cu"))]
+    for n in ("cache_part", "umma_load", "umma_logits", "umma_sums", "umma_softmax", "tree_part"):
+        assert n in names
+    body = dict(functions(os.path.join(protocols.CSRC, "tree_tc.cu")))["umma_softmax"]
+    assert len(re.findall(protocols.WAIT, body)) >= 5 and len(BARRIER.findall(body)) >= 4
+    assert "join_rows_of" in [n for n, _ in functions(os.path.join(protocols.CSRC, "tree_common.cuh"))]
+
+
+def test_arrivals_count(monkeypatch):
+    ok = "bool ok = wait_all(&a, 0, f); "
+    monkeypatch.setattr(protocols, "BARRIER", BARRIER)
+    assert protocols.barriers_behind_a_wait(ok + "if (ok) tc::named_barrier_arrive(5, 192);")
+    assert protocols.barriers_behind_a_wait("{" + ok + "if (!ok) return; tree::cluster_arrive(); }")
+    assert not protocols.barriers_behind_a_wait(ok + "if (ok) x(); cluster_arrive();")
