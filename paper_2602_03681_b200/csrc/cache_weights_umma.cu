@@ -153,6 +153,8 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
         }
         __syncwarp();
     } else {                                      // ---- the sums ----
+        // (Who has given up announces nothing any more: arrivals without the waits between them would let the copies' warp take
+        // places for free whose copies are in flight, and arm their barriers a second time.)
         const int g = warp >> 2, r = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         bool ok = true;
@@ -174,7 +176,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
 #pragma unroll
                     for (int c = 0; c < kSlices; ++c) row_squares<D, G>(dyn_u + c * kQSlice, c, t, ss);
                     f *= rsqrtf(ss[G == 2 ? s : 0] / ds + norm_eps);
-                    mbar_arrive(&bar.q_empty);
+                    if (ok) mbar_arrive(&bar.q_empty);
                 }
                 s_row[tid] = make_float2(f, l * kLog2e);
                 s_vis[tid] = vis;
@@ -196,7 +198,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         const int i = kSlices * u + c;
                         ok = ok && wait_all(&bar.full[i % kStages], (i / kStages) & 1, abort_flag);
                         row_squares<D, G>(ring + i % kStages * kSlice, c, r, ss);
-                        mbar_arrive(&bar.empty[i % kStages]);
+                        if (ok) mbar_arrive(&bar.empty[i % kStages]);
                     }
 #pragma unroll
                     for (int s = 0; s < G; ++s) fk[s] = rsqrtf(ss[s] / ds + norm_eps);
@@ -231,7 +233,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         }
                     }
                 tc_fence_before_sync();
-                mbar_arrive(&bar.free[place_of(u)]);
+                if (ok) mbar_arrive(&bar.free[place_of(u)]);
                 // (no status word: a wait that has run out shows as a NaN)
                 if (mine) *at = ok && !abort_flag[0] ? was + ((sum[0] + sum[1]) + (sum[2] + sum[3])) : NAN;
             }

@@ -57,3 +57,57 @@ def test_arrivals_count(monkeypatch):
     assert protocols.barriers_behind_a_wait(ok + "if (ok) tc::named_barrier_arrive(5, 192);")
     assert protocols.barriers_behind_a_wait("{" + ok + "if (!ok) return; tree::cluster_arrive(); }")
     assert not protocols.barriers_behind_a_wait(ok + "if (ok) x(); cluster_arrive();")
+
+
+def arrivals_in_spite_of_a_wait(body):
+    """The arrivals on an mbarrier that a thread makes behind a bounded wait, however that ended: neither their statement nor a
+    block around it asks for the outcome, and no way out that does lies before them.  Arrivals without the waits between
+    them run ahead of what they stand for: a ring's place passes for free while a copy into it is in flight, and the barrier of
+    that copy is armed a second time.  (Those on places, which are named empty or free; a barrier of one phase has nothing to
+    run ahead of.)"""
+    wait = protocols.WAIT
+    outcomes = set(re.findall(r"(\w+)\s*=[^=;{}]*" + wait, body))
+    while outcomes:
+        more = set(re.findall(r"(\w+)\s*=[^=;{}]*\b(?:%s)\b" % "|".join(outcomes), body))
+        if more <= outcomes:
+            break
+        outcomes |= more
+    decided = re.compile(wait + "".join(r"|\b%s\b" % n for n in sorted(outcomes)))
+    found, stack, start, i, waited = [], [False], 0, 0, False
+    while i < len(body):
+        if body[i] == "(":
+            depth = 1
+            while depth:
+                i += 1
+                depth += {"(": 1, ")": -1}.get(body[i], 0)
+        if body[i] in "{;}":
+            words = body[start:i]
+            asks = bool(re.search(r"\b(if|while|for)\s*\(|&&", words)) and bool(decided.search(words))
+            if re.search(r"\bmbar_arrive\s*\([^;]*(?:empty|\bfree)\b", words) and waited and not asks and not any(stack):
+                found.append(" ".join(words.split()))
+            waited |= bool(re.search(wait, words))
+            if asks and re.search(r"\b(break|continue|return)\b", words):
+                stack[-1] = True                              # (the rest of this block)
+            if body[i] == "{":
+                stack.append(asks)
+            elif body[i] == "}" and len(stack) > 1:
+                stack.pop()
+            start = i + 1
+        i += 1
+    return found
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_who_has_given_up_announces_nothing(source):
+    path = os.path.join(protocols.CSRC, source)
+    for name, body in protocols.kernels(path) + functions(path):
+        assert not arrivals_in_spite_of_a_wait(body), name
+
+
+def test_the_rule_on_arrivals_finds_what_it_is_for():
+    assert arrivals_in_spite_of_a_wait("ok = ok && wait_all(&f, 0, a); x(); mbar_arrive(&empty);")
+    assert arrivals_in_spite_of_a_wait("for (;;) { if (n) { ok = wait_all(&f, 0, a) && ok; mbar_arrive(&empty); } }")
+    assert not arrivals_in_spite_of_a_wait("ok = ok && wait_all(&f, 0, a); if (ok) mbar_arrive(&empty);")
+    assert not arrivals_in_spite_of_a_wait("ok = ok && wait_all(&f, 0, a); if (ok) { x(); mbar_arrive(&empty); }")
+    assert not arrivals_in_spite_of_a_wait("for (;;) { if (!wait_all(&f, 0, a)) break; mbar_arrive(&empty); }")
+    assert not arrivals_in_spite_of_a_wait("mbar_arrive(&empty); ok = wait_all(&f, 0, a);")
