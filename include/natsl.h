@@ -435,11 +435,14 @@ uint64_t natsl_launch_count(void);
 /*
  * Test hook for the time-out path (no counterpart in the paper).  Every device-side wait of the
  * tensor-core kernels is bounded (about two seconds by default); when a wait runs out the kernel
- * records NATSL_ERR_TIMEOUT in the status word, waits for its own copies in flight, frees its
- * tensor memory and returns.  This call sets, for all following forward calls of the process,
+ * records NATSL_ERR_TIMEOUT in the status word (natsl_cache_weights, which has none: NaN in the
+ * entries), waits for its own copies in flight, frees its tensor memory and returns.  This call sets,
+ * for all following calls of the process,
  *   kcycles              the bound in units of 1024 clock cycles (0: back to the default), and
- *   withhold_scan_flags  non-zero: the scan does not raise the per-chunk counters the softmax
- *                        kernel's epilogue waits for, so that exactly this wait runs out.
+ *   withhold_scan_flags  non-zero: the forward's scan does not raise the per-chunk counters the softmax
+ *                        kernel's epilogue waits for, so that exactly this wait runs out; the tree step
+ *                        beyond 32 nodes does not announce its probabilities, and the cache weights of
+ *                        more than 16 rows neither their logits nor the places that are free again.
  * Nothing faults and nothing hangs: the call returns after the bound and reports the time-out.
  */
 void natsl_debug_set_wait_limit(uint32_t kcycles, int withhold_scan_flags);

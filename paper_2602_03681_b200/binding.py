@@ -259,7 +259,8 @@ def natsl_static_status() -> int:
 
 def natsl_debug_set_wait_limit(kcycles: int, withhold_scan_flags: bool = False):
     """Test hook: bound of the device-side waits in units of 1024 cycles (0 = default) and whether
-    the scan withholds the per-chunk flags the softmax kernel waits for."""
+    the scan withholds the per-chunk flags the softmax kernel waits for, the tree step and the cache
+    weights on tcgen05 the arrivals that natsl.h names."""
     lib().natsl_debug_set_wait_limit(int(kcycles), 1 if withhold_scan_flags else 0)
 
 

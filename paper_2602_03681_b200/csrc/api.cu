@@ -12,10 +12,11 @@ using namespace natsl;
 
 namespace natsl {
 // Test hooks (natsl_debug_set_wait_limit): a bound for the device-side waits of the following
-// launches, and whether the scan withholds the per-chunk flags the softmax kernel waits for.
+// launches, and whether arrivals that other warps or kernels wait for are withheld.
 static std::atomic<uint32_t> g_debug_wait_kcycles{0};
 static std::atomic<int> g_debug_withhold_flags{0};
 int debug_wait_kcycles() { return (int)g_debug_wait_kcycles.load(std::memory_order_relaxed); }
+int debug_withhold() { return g_debug_withhold_flags.load(std::memory_order_relaxed); }
 static std::atomic<uint64_t> g_launches{0};
 void count_launch(int n) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
 }  // namespace natsl
@@ -570,7 +571,7 @@ int natsl_hybrid_fwd(const void *q, const void *k, const void *v, const float *g
         NATSL_TRY(mark());
         NATSL_TRY(beside ? gather() : prepare());
         NATSL_TRY(mark());
-        int32_t *flags_scan = beside && !g_debug_withhold_flags.load(std::memory_order_relaxed) ? f.emit_flags : nullptr;
+        int32_t *flags_scan = beside && !debug_withhold() ? f.emit_flags : nullptr;
         const int32_t *flags_softmax = beside ? f.emit_flags : nullptr;
         const ScanOut so{f.o_la16, p->o_la, flags_scan};
         if (nseg > 1) {   // few (batch, head) pairs: segments in parallel, chained by their transitions

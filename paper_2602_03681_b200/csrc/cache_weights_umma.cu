@@ -46,12 +46,13 @@ template <int D, int G> __device__ __forceinline__ void row_squares(const uint8_
     }
 }
 
+// withhold (a test's): neither logits nor free places are announced, so that what waits for them gives up.
 template <int D, int G, bool kNorm>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                           const float *__restrict__ lse, const int32_t *__restrict__ visible, const int32_t *__restrict__ cache_len,
                           int cap, float *__restrict__ weight, int H, int T, float scale, float norm_eps, int runs, int run,
-                          int wait_kcycles) {
+                          int wait_kcycles, int withhold) {
     constexpr int ds = D / G, kSlices = D / 64, kCols = kRows * G;       // kCols: columns of a tile's logits
     extern __shared__ __align__(1024) uint8_t dyn_u[];    // q, slice by slice; then the ring
     __shared__ Bars bar;
@@ -140,7 +141,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         mma_ss(ts + (c * 64 + k * 16) / ds * 64, desc_kmajor(ak + k * 32), desc_kmajor(aq + c * kQSlice + k * 32), idesc,
                                (c * 64 + k * 16) % ds != 0);
                     mma_commit(&bar.empty[s]);
-                    if (c == kSlices - 1) mma_commit(&bar.s[place]);
+                    if (c == kSlices - 1 && !withhold) mma_commit(&bar.s[place]);
                     if (c == kSlices - 1 && t == nt - 1) mma_commit(&bar.q_empty);
                 }
                 __syncwarp();
@@ -233,7 +234,7 @@ cache_weights_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __gri
                         }
                     }
                 tc_fence_before_sync();
-                if (ok) mbar_arrive(&bar.free[place_of(u)]);
+                if (ok && !withhold) mbar_arrive(&bar.free[place_of(u)]);
                 // (no status word: a wait that has run out shows as a NaN)
                 if (mine) *at = ok && !abort_flag[0] ? was + ((sum[0] + sum[1]) + (sum[2] + sum[3])) : NAN;
             }
@@ -259,7 +260,8 @@ cudaError_t launch(const CUtensorMap &map_q, const CUtensorMap &map_k, const flo
     cudaError_t e = allow_smem(kernel, kSmem);
     if (e != cudaSuccess) return e;
     e = launch_kernel(kernel, dim3((unsigned)(BH * runs)), dim3(kThreads), kSmem, st, true, map_q, map_k, lse, visible, cache_len, cap,
-                      weight, s.H, s.L, scale, norm_eps, runs, run, debug_wait_kcycles());
+                      weight, s.H, s.L, scale, norm_eps, runs, run, debug_wait_kcycles(),
+                      debug_withhold());
     count_launch();
     return e;
 }

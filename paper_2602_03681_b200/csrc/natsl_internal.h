@@ -143,6 +143,8 @@ int sm_count();   // multiprocessors of the current device (cached per device)
 // Bound of the device-side waits in units of 1024 cycles, 0 = the default (about two seconds);
 // non-zero only after natsl_debug_set_wait_limit.  Every tensor-core kernel launch passes it on.
 int debug_wait_kcycles();
+// Whether kernels are to hold back the arrivals that natsl_debug_set_wait_limit names.
+int debug_withhold();
 
 // softmax_bwd_tc.cu -- tensor-core backward of the softmax branch (bf16 storage).  Qh is the softmax operation's
 // fp16 copy of q [B,H,L,d]; dO16 the fp16 branch-output gradient [B,H,L,d]; k16, v16 the

@@ -476,9 +476,10 @@ __device__ void umma_sums(const UmmaShare<D> &in, uint32_t tmem) {
     umma_drain(&bar->drain[1]);
 }
 
-// The four softmax warps: thread = row of a key group.
+// The four softmax warps: thread = row of a key group.  withhold (a test's): no tile's probabilities are announced, so that
+// what waits for them gives up.
 template <int D, int G, bool kNorm>
-__device__ void umma_softmax(const Args &a, typename Layout<D, 4>::S *sums, const UmmaShare<D> &in, uint32_t tmem, int n_nodes) {
+__device__ void umma_softmax(const Args &a, typename Layout<D, 4>::S *sums, const UmmaShare<D> &in, uint32_t tmem, int n_nodes, bool withhold) {
     using namespace tc;
     using L = Layout<D, 4>;
     constexpr int ds = D / G, kSlices = D / 64;
@@ -602,7 +603,7 @@ __device__ void umma_softmax(const Args &a, typename Layout<D, 4>::S *sums, cons
             }
         }
         tc_fence_before_sync();
-        if (ok) mbar_arrive(&bar->p[place_of<G>(t)]);
+        if (ok && !withhold) mbar_arrive(&bar->p[place_of<G>(t)]);
     }
     const int t_last = g + 2 * (i - 1);           // (products are done in their order)
     if (ok && i > 0) ok = wait_all(&bar->o[place_of<G>(t_last)], place_phase<G>(t_last), abort_flag);
@@ -1000,7 +1001,8 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
 
 template <int D, int G, bool kNorm, int R>
 __global__ void __launch_bounds__(Layout<D, R>::kThreads, Layout<D, R>::kCtas)
-tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, Args a, int wait_kcycles) {
+tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, Args a, int wait_kcycles,
+               int withhold) {
     using L = Layout<D, R>;
     constexpr int kReaders = L::kReaders, kThreads = L::kThreads;
     extern __shared__ __align__(1024) uint8_t dyn_tc[];
@@ -1065,7 +1067,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant_
         const int keys = share.to - share.from;
         const UmmaShare<D> u{{&map_k, &map_v}, &bars, dyn_tc, dyn_tc + L::oRing, bh * a.cap + share.from, keys, (keys + kTileKeys - 1) / kTileKeys};
         if (tid < 128) {
-            umma_softmax<D, G, kNorm>(a, sums, u, tmem, n);
+            umma_softmax<D, G, kNorm>(a, sums, u, tmem, n, withhold != 0);
         } else if (tid < 160) {
             umma_sums<D, G>(u, tmem);
             tc::named_barrier_sync(5, 192);
@@ -1095,7 +1097,7 @@ cudaError_t launch(const Args &a, int BH, cudaStream_t st) {
                                 !tch::make_map_2d(&map_v, a.v_cache, (uint64_t)BH * a.cap, D, kTileKeys)))
         return cudaErrorInvalidValue;
     return launch_clusters(kernel, BH * a.cluster, a.cluster, Layout<D, R>::kThreads, Layout<D, R>::kTotal, st, map_k, map_v, a,
-                           debug_wait_kcycles());
+                           debug_wait_kcycles(), debug_withhold());
 }
 template <int D, int G, bool kNorm>
 cudaError_t by_rows(const Args &a, int BH, cudaStream_t st) {
