@@ -459,6 +459,19 @@ __device__ void umma_sums(const UmmaShare<D> &in, uint32_t tmem) {
         const int place = place_of<G>(t);
         ok = wait_all(&bar->full[1][in.stage(1, t)], in.phase(1, t), bar->abort) && wait_all(&bar->p[place], place_phase<G>(t), bar->abort);
         if (!ok) break;
+        // Rows past the end count as zeros: what lies there may be anything.  (This warp follows every phase of V's barriers.  The
+        // softmax warps, which do not, are up to four tiles ahead with one softmax head, V has three places at 128 columns: to
+        // them the barrier's last phase but one looks like the one to come, and they cleared rows of a tile on its way.)
+        const int left = in.keys - t * kTileKeys;
+        if (left < kTileKeys) {
+            uint8_t *tile = in.at(1, t);
+            for (int e = threadIdx.x & 31; e < (kTileKeys - left) * (D / 8); e += 32) {
+                const int c = e % (D / 8), j = left + e / (D / 8);
+                *reinterpret_cast<uint4 *>(tile + c / 8 * in.kSlice + j * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+        }
         tc_fence_after_sync();
         const uint32_t av = uniform(smem_u32(in.at(1, t))), ts = tm + 64 * place, to = tm + kTmemO + 128 * (t & 1);
         if (elect_one()) {
@@ -591,17 +604,6 @@ __device__ void umma_softmax(const Args &a, typename Layout<D, 4>::S *sums, cons
             }
         }
         tmem_wait_st();
-        if (left < kTileKeys && ok) {             // rows past the end count as zeros: what lies there may be anything
-            ok = wait_all(&bar->full[1][in.stage(1, t)], in.phase(1, t), abort_flag);
-            if (ok) {
-                uint8_t *tile = in.at(1, t);
-                for (int e = r; e < (kTileKeys - left) * (D / 8); e += 64) {
-                    const int c = e % (D / 8), j = left + e / (D / 8);
-                    *reinterpret_cast<uint4 *>(tile + c / 8 * in.kSlice + j * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async_smem();
-            }
-        }
         tc_fence_before_sync();
         if (ok && !withhold) mbar_arrive(&bar->p[place_of<G>(t)]);
     }

@@ -500,3 +500,47 @@ def test_any_logit_scale(dtype, G, norm, T, sm, monkeypatch):
     monkeypatch.setattr(test_gpu_tree, "scales", lambda d, G, norm: (d ** -0.5, sm))
     x = make(3, 1, 2, T, 128, [50, 3], 50, dtype, route="all", unit=not norm)
     check(call(x, dtype, G=G, norm=norm), reference(x, G, norm), dtype)
+
+
+@pytest.mark.parametrize("d,G", [(128, 1), (128, 2), (64, 1)])
+@pytest.mark.parametrize("T", [33, 64])
+def test_full_trees_one_behind_the_other(d, G, T):
+    """More pairs than are resident at once over long caches of every length modulo the tile, two batches in turns and nothing waited
+    for between them: the same bits as alone.  Behind the lengths lies what may not be seen."""
+    from paper_2602_03681_b200 import binding
+    B, H, cap = 8, 16, 4000
+    dev_gen = torch.Generator(device="cuda").manual_seed(T + d + G)
+    la, sm = scales(d, G, False)
+
+    def batch():
+        def rows(*s):
+            return torch.nn.functional.normalize(torch.randn(s, generator=dev_gen, device="cuda"), dim=-1).bfloat16()
+        t = dict(q=rows(B, T, H, d), k=rows(B, T, H, d), v=rows(B, T, H, d), k_cache=rows(B, H, cap, d), v_cache=rows(B, H, cap, d))
+        t["g"], t["beta"] = -torch.rand(B, T, H, generator=dev_gen, device="cuda"), torch.rand(B, T, H, generator=dev_gen, device="cuda")
+        t["route"] = torch.randint(0, 3, (B, T, H), generator=dev_gen, device="cuda").to(torch.uint8)
+        t["parent"] = (torch.arange(T, device="cuda", dtype=torch.int32) - 2).clamp(min=-1).repeat(B, 1)
+        t["state"] = torch.randn(B, H, d, d, generator=dev_gen, device="cuda")
+        t["cache_len"] = (cap - torch.randint(0, cap // 2, (B, H), generator=dev_gen, device="cuda")).to(torch.int32)
+        behind = torch.arange(cap, device="cuda") >= t["cache_len"][:, :, None]
+        t["k_cache"][behind], t["v_cache"][behind] = float("inf"), float("nan")
+        t["n_nodes"], t["out"], t["u"] = None, torch.empty_like(t["q"]), torch.empty(B, T, H, d, device="cuda")
+        t["lse"] = torch.empty((B, H, G, T) if G > 1 else (B, H, T), device="cuda")
+        t["p"] = binding.make_params(B, H, T, d, binding.NATSL_BF16, la, sm, lse=t["lse"], G=G)
+        t["ws"] = binding.alloc_workspace(t["p"], binding.OP_TREE)
+        return t
+
+    one, other = batch(), batch()
+    alone = []
+    for t in (one, other):
+        step(t)
+        torch.cuda.synchronize()
+        alone.append([t[m].clone() for m in ("out", "u", "lse")])
+        assert all(torch.isfinite(y).all() for y in alone[-1])
+    for _ in range(40):
+        for _ in range(5):
+            step(one)
+            step(other)
+        torch.cuda.synchronize()
+        for t, want in zip((one, other), alone):
+            assert all(torch.equal(t[m], y) for m, y in zip(("out", "u", "lse"), want))
+    assert binding.natsl_device_status(one["ws"]) == 0 and binding.natsl_device_status(other["ws"]) == 0
