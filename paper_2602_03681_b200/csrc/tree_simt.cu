@@ -358,13 +358,16 @@ cudaError_t launch_tree_step(const TreeCall &c, Shape s, HeadGroups hg, bool ten
     const int BH = s.B * s.H;
     // CTAs per pair: as many as can be resident for all pairs at once.  A cluster lies within one of the GPU's groups of 16 to 18
     // multiprocessors, so 148 of them hold 15 clusters of eight or 33 of four, twice that where a multiprocessor holds two CTAs
-    // (up to 32 nodes).  Pairs over 1638 keys of 128 columns, eight / four: 64 nodes of 16 pairs 31 / 19 us, of 8 17 / 18.5; 16
-    // nodes of 28 pairs 11.3 / 12.3, 32 of 32 17.9 / 16.0; four / two: 64 nodes of 33 pairs 20 / 25, of 48 37 / 26; 16 nodes of
-    // 60 15 / 17, of 71 17.1 / 17.3.  With four softmax heads of 32 columns four at least: a CTA's columns belong to one of them.
-    const int per = s.L > 32 ? 1 : 2, cluster = BH <= 14 * per ? 8 : BH <= 33 * per || hg.G == 4 ? 4 : 2;
+    // (tensor cores, up to 32 nodes).  Pairs over 1638 keys of 128 columns, eight / four: 64 nodes of 16 pairs 31 / 19 us, of 8 17 /
+    // 18.5; 16 nodes of 28 pairs 11.3 / 12.3, 32 of 32 17.9 / 16.0; four / two: 64 nodes of 33 pairs 20 / 25, of 48 37 / 26; 16 nodes
+    // of 60 15 / 17, of 71 17.1 / 17.3.  The CUDA-core kernel has one CTA per multiprocessor throughout: fp32 pairs over 1024 keys,
+    // eight / four: 2 nodes of 20 pairs 28 / 25, 16 of 20 55 / 50, 32 of 28 101 / 93; four / two: 2 nodes of 40 47 / 44, 16 of 64 105 /
+    // 102, 32 of 40 184 / 179.  With four softmax heads of 32 columns four at least: a CTA's columns belong to one of them.
+    const bool on_tensor_cores = tensor_cores && hg.G <= 2;
+    const int per = on_tensor_cores && s.L <= 32 ? 2 : 1, cluster = BH <= 14 * per ? 8 : BH <= 33 * per || hg.G == 4 ? 4 : 2;
     const Args a{c.q, c.k, c.v, c.g, c.beta, c.route, c.parent, c.n_nodes, c.w, c.state, c.k_cache, c.v_cache, c.cache_len,
                  c.out, c.u, c.lse, (int32_t *)c.ws, s.H, s.L, c.cap, hg.G, cluster, c.scale_la, c.scale_sm, c.eps, hg.norm_eps};
-    if (tensor_cores && hg.G <= 2) return launch_tree_tc(a, BH, s.d, st);
+    if (on_tensor_cores) return launch_tree_tc(a, BH, s.d, st);
     if (s.bf16) return s.d == 128 ? by_rows<__nv_bfloat16, 128>(a, BH, st) : by_rows<__nv_bfloat16, 64>(a, BH, st);
     return s.d == 128 ? by_rows<float, 128>(a, BH, st) : by_rows<float, 64>(a, BH, st);
 }
