@@ -342,7 +342,7 @@ int natsl_decode_block_end(const uint8_t *route_block, const float *g_block, flo
  * paper generates one token at a time, which is the tree of one node).  A draft model proposes p->L tokens
  * per sequence, 1 <= p->L <= 64, as a tree: token i follows token parent[b,i] of the same sequence, or, with
  * -1, the context that `state` and the cache hold.  Every node gets the output that natsl_decode_step would
- * give it after its ancestors: the delta rule runs along its path, and its softmax reads the cache and the
+ * give it after its ancestors, up to rounding (below): the delta rule runs along its path, and its softmax reads the cache and the
  * retained tokens of its path.  Routes as in natsl_decode_step: 0 folded into the state, 1 retained, 2 both
  * (a token of a block whose decision is open).  Nothing is updated: natsl_tree_commit does that for the path
  * that was accepted.
@@ -360,6 +360,11 @@ int natsl_decode_block_end(const uint8_t *route_block, const float *g_block, flo
  * p->G in {1, 2, 4} with d / G >= 32 and NATSL_QK_NORM as in natsl_decode_step.  bf16 storage runs on the
  * tensor cores, except with NATSL_FORCE_SIMT or four softmax heads.  A parent that is not below its node
  * counts as -1 and is reported as NATSL_ERR_TREE, like a count outside [0, L] (the nearer of both).
+ * Precision: u, the log-sum-exps and the softmax's sums are fp32 throughout.  On the tensor cores `out` is made
+ * with fewer bits than natsl_decode_step's, which is fp32 up to its last rounding: the probabilities meet V
+ * rounded to bf16 (2^-8 of each at most; together with the rounding to storage `out` is 2.1e-3 off in the
+ * 2-norm, where that rounding alone takes 1.7e-3), and the linear read-out takes u and its coefficients as two
+ * bf16 terms each (2^-16).  NATSL_FORCE_SIMT keeps fp32 here too.
  * ws holds natsl_workspace_size(p, NATSL_OP_TREE) bytes (the status word of natsl_device_status alone, TIMEOUT
  * among its values), is zero-filled once before its first use and is not shared by calls that overlap on the
  * GPU.  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, UNSUPPORTED, CUDA.
@@ -399,7 +404,10 @@ int natsl_tree_commit(const void *k, const void *v, const float *g, const uint8_
  *   k_cache [B,H,cache_cap,d], cache_len [B,H]: read (a length outside [0, cache_cap] counts as the nearer of
  *       both); weight [B,H,cache_cap] fp32: updated in place, entries from the length on are left alone.
  * NATSL_QK_NORM and p->G as in natsl_tree_step.  No workspace, and so no status word: should a wait inside the
- * kernel run out, entries get a NaN.  Errors: NULL, SHAPE, DTYPE, ALIGN, UNSUPPORTED, CUDA.
+ * kernel run out, entries get a NaN.  An entry's sum starts from what `weight` holds at its place when its first
+ * rows are weighed: where K/V are appended to a cache that was cut down before, that is what an entry of old has
+ * left there, so the caller sets `weight` to zero from the length on, after natsl_cache_evict or ahead of the
+ * entry's first rows.  Errors: NULL, SHAPE, DTYPE, ALIGN, UNSUPPORTED, CUDA.
  */
 int natsl_cache_weights(const void *q, const float *lse, const int32_t *visible, const void *k_cache,
                         const int32_t *cache_len, int32_t cache_cap, float *weight, const natsl_params *p,
@@ -409,9 +417,9 @@ int natsl_cache_weights(const void *q, const float *lse, const int32_t *visible,
  * Eviction: every (sequence, head) with more than `keep` entries keeps `keep` of them -- the first `first`,
  * the last `recent` and, of those between, the ones of the highest weight (ties: the lower index; a NaN
  * counts as the lowest weight) -- moved to the front in their order; cache_len becomes `keep`.  Others are
- * left untouched.
+ * left untouched (a length outside [0, cache_cap] counts as the nearer of both).
  *   k_cache,v_cache [B,H,cache_cap,d] in p->dtype, weight [B,H,cache_cap] fp32, cache_len [B,H] i32: updated
- *       in place; rows from the new length on are left as they were;
+ *       in place; rows from the new length on are left as they were, their weights too (natsl_cache_weights);
  *   kept [B,H,keep] i32: the former places of the entries that are now 0 .. cache_len - 1.
  * 1 <= keep <= cache_cap, first >= 0, recent >= 0, first + recent <= keep.  Of p only B, H, d, C, dtype, eps
  * count (the last two must be valid).  No workspace.  Errors: NULL, SHAPE, DTYPE, ALIGN, CUDA.

@@ -390,3 +390,41 @@ def test_offsets_past_32_bits(dtype, T):
         del kc, vc, weight
         torch.cuda.empty_cache()
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dtype,T", [("f32", 6), ("bf16", 6), ("bf16", 40)])
+def test_weights_of_what_is_appended_after_an_eviction(dtype, T):
+    """The places behind a cut cache keep the weights of what lay there; set to zero, as natsl.h asks, they give the entries that
+    are appended next the weights that these rows give them and no others."""
+    from paper_2602_03681_b200 import binding
+    B, H, d, cap, keep = 1, 3, 64, 200, 50
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = make(T, B, H, T, d, [150, 90, 51], cap, dtype, tree="chain", route=1)
+    x["path"][:], x["n_path"][:] = np.arange(T), T
+    t = {n: dev(x[n], dt if n in ("q", "k", "v", "k_cache", "v_cache") else None) for n in x if x[n] is not None}
+    kc, vc, n, state = t["k_cache"], t["v_cache"], t["cache_len"], t["state"]
+    la, sm = scales(d, 1, False)
+    weight = torch.rand(B, H, cap, device="cuda") + 1.0
+    kept = torch.empty(B, H, keep, dtype=torch.int32, device="cuda")
+    out, u = torch.empty_like(t["q"]), torch.empty(B, T, H, d, device="cuda")
+    lse = torch.empty(B, H, T, device="cuda")
+    p = binding.make_params(B, H, T, d, binding._dtype_code(out), la, sm, lse=lse)
+    ws = binding.alloc_workspace(p, binding.OP_TREE)
+    binding.natsl_cache_evict(kc, vc, weight, n, keep, 2, 5, kept, p)
+    behind = torch.arange(cap, device="cuda") >= n[:, :, None]
+    assert (weight[behind] >= 1.0).all()             # (as they were)
+    weight.masked_fill_(behind, 0.0)
+    binding.natsl_tree_step(t["q"], t["k"], t["v"], t["g"], t["beta"], t["route"], t["parent"], None, state, kc, vc, n, out, u, p, ws)
+    binding.natsl_tree_commit(t["k"], t["v"], t["g"], t["route"], u, t["path"], t["n_path"], state, kc, vc, n, p, ws)
+    visible = (keep + torch.arange(1, T + 1, device="cuda", dtype=torch.int32))[None, :, None].expand(B, T, H).contiguous()
+    before = weight.clone()
+    binding.natsl_cache_weights(t["q"], lse, visible, kc, n, weight, p)
+    assert binding.natsl_device_status(ws) == 0 and (n == keep + T).all()
+    # a row of a chain sees the cache and itself with what lies before it: all of its unit goes to entries
+    given = (weight - before)[:, :, :keep + T].double()
+    assert torch.equal(weight[:, :, keep + T:], before[:, :, keep + T:])
+    assert (given.sum(-1) - T).abs().max() <= 1e-4 * T
+    ref = tree.cache_weights(x["q"], lse.double().cpu().numpy()[:, :, None], visible.cpu().numpy(), kc.double().cpu().numpy(),
+                             n.cpu().numpy(), np.zeros((B, H, cap)), scale_sm=sm)[:, :, keep:keep + T]
+    got = weight[:, :, keep:keep + T].cpu().numpy()
+    assert (np.abs(got - ref) <= 1e-4 * (ref + np.sqrt((ref ** 2).mean()))).all()
