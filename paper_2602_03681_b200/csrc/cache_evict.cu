@@ -7,9 +7,10 @@
 // natsl_cache_evict keeps the first entries, the latest ones and the heaviest of the rest (a radix select on the
 // weights' bits finds the threshold; ties to the lowest index) and moves them to the front, in order and in place.
 //
-// B200: the weights of 64 x 16 caches of 1638 entries of 128 columns for up to 16 rows 72 us (444 MB: 6.2 TB/s, 94 % of a
-// copy's rate); one pass of eviction over 64 x 16 caches of 1638 150 us at its first call (up to 1.09 GB, entries before the
-// first gap stay) and 39 us where only the latest entries move; 16 caches of 8192 entries 34 us and 20 us.
+// B200 (a range is what several of them gave): the weights of 64 x 16 caches of 1638 entries of 128 columns for up to 16 rows 72 to
+// 75 us (444 MB: 5.9 to 6.2 TB/s, 91 to 94 % of a copy's rate); an eviction over 64 x 16 caches of up to 1638 150 to 184 us (up to
+// 1.09 GB, entries before the first gap stay), and 39 to 44 us where it has been cut already and only the latest entries move; of 16
+// caches of 8192 entries 34 to 35 us, and 20 to 23.
 #include <algorithm>
 #include "common.cuh"
 #include "natsl_internal.h"

@@ -8,7 +8,7 @@
 // one for 16 exponentials.  Two CTAs per multiprocessor, each with 64 rows of q at a time as the B operand and a ring of five
 // slices of K (128 keys, 64 columns).  Two groups of four warps take tiles in turns; one warp issues copies, one MMAs.
 //
-// B200: 64 rows, two heads, 4 x 16 caches of up to 3277 keys 20 us: of a CTA's 24000 cycles 12300 are the exponentials of its
+// B200: 64 rows, two heads, 4 x 16 caches of up to 3277 keys 20 to 21 us: of a CTA's 24000 cycles 12300 are the exponentials of its
 // multiprocessor, 4000 the start up to the rows' factors.  Against warp-level MMAs with the rows in registers, 64 x 16 caches of
 // up to 1638 keys of 128 columns, one head / two normalised: 16 rows 62 / 80 us where those take 59 / 70; 17 rows 62 / 80 and
 // 70 / 99, 64 rows 65 / 106 and 92 / 135, 128 rows 107 / 201 and 171 / 258.

@@ -5,7 +5,7 @@
 //
 // Bound by the state's round trip (8 d^2 bytes per pair).  One CTA per pair, four per multiprocessor: a thread has four columns
 // and kRows neighbouring rows, read before the path is, four rows at a time afterwards.  B200: 64 x 16 pairs of 128 columns,
-// paths of up to 32 nodes, 37 us (146 MB: 3.9 TB/s; a wave of CTAs is short, and each begins with the chain length of the
+// paths of up to 32 nodes, 37 to 39 us (146 MB: 3.8 to 3.9 TB/s; a wave of CTAs is short, and each begins with the chain length of the
 // path -> rows -> products); one CTA per multiprocessor with the state in registers took 64 us.  16 pairs take 5.4 us.
 #include "tree_common.cuh"
 

@@ -17,9 +17,10 @@
 // Zeros in the place of what a node does not see would let an infinity or a NaN through, so values that are not finite take
 // a slower way that looks at the paths.
 //
-// B200: one token of 64 x 16 heads over 1638 keys 155 us (930 MB: 6.0 TB/s, 92 % of a copy's rate); 32 nodes 216 us (4.5 TB/s:
-// of a CTA's 53000 cycles the last 10000 are the join, which no load overlaps but the neighbour CTA's); 64 nodes of 8 x 16
-// heads over up to 6554 keys 92 us (161 us with warp-level MMAs; with 64 columns 67 and 106); 16 nodes of 16 heads 11 us.
+// B200 (a range is what several of them gave): one token of 64 x 16 heads over 1638 keys 155 to 166 us (930 MB: 5.6 to 6.0 TB/s,
+// 86 to 92 % of a copy's rate); 32 nodes 216 to 236 us (4.1 to 4.5 TB/s: of a CTA's 53000 cycles the last 10000 are the join, which
+// no load overlaps but the neighbour CTA's); 64 nodes of 8 x 16 heads over up to 6554 keys 91 to 95 us (161 us with warp-level MMAs;
+// with 64 columns 63 to 67, and 100 to 106); 16 nodes of 16 heads 11 us.
 #include <algorithm>
 #include "tree_common.cuh"
 
@@ -828,8 +829,7 @@ __device__ void tree_part(const Args &a, typename Layout<D, R>::S *sums, uint8_t
                 for (int m0 = 0; m0 < 2 * R; m0 += kM) {
                     uint32_t af[kM][4];
 #pragma unroll
-                    for (int m = 0; m < kM; ++m)
-{
+                    for (int m = 0; m < kM; ++m) {
                             const int t = (m0 + m) % R * 16 + (lane & 15), c = 2 * k + (lane >> 4);
                             ldmatrix_x4(m0 + m < R ? k_at + t * L::kPitch + c * 16 : q_at + L::q_piece(t, c), af[m]);
                         }
